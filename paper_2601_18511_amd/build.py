@@ -9,10 +9,11 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 # translation units of the library (each holds its own kernels; no device code crosses files)
-SOURCES = [os.path.join(CSRC, n) for n in ("pcmm.hip", "pcmm_shortk.hip", "pcmm_resident.hip", "pcmm_slot.hip", "pcmv.hip")]
+SOURCES = [os.path.join(CSRC, n) for n in ("pcmm.hip", "pcmm_shortk.hip", "pcmm_resident.hip", "pcmm_slot.hip", "pcmv.hip", "ppmv.hip", "ppkv.hip")]
 SRC = SOURCES[0]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "pcmm.h")
-INTERNAL_HEADERS = [os.path.join(CSRC, n) for n in ("pcmm_host.hpp", "pcmm_device.hpp", "pcmm_shortk.hpp", "pcmm_resident.hpp", "pcmm_hip_util.hpp", "pcmv_host.hpp")]
+CLEAR_HEADER = os.path.join(os.path.dirname(_HERE), "include", "ppmm.h")
+INTERNAL_HEADERS = [os.path.join(CSRC, n) for n in ("pcmm_host.hpp", "pcmm_device.hpp", "pcmm_shortk.hpp", "pcmm_resident.hpp", "pcmm_hip_util.hpp", "pcmv_host.hpp", "ppmm_host.hpp", "ppmm_device.hpp")]
 LIB = os.path.join(_HERE, "libpcmm.so")
 STAMP = LIB + ".stamp"          # digest of the sources and flags the library was built from
 
@@ -39,7 +40,7 @@ def hipcc_path() -> str:
 def source_digest() -> str:
     """Digest of everything the library is built from: the sources, the headers and the flags."""
     h = hashlib.sha256()
-    for path in SOURCES + INTERNAL_HEADERS + [HEADER]:
+    for path in SOURCES + INTERNAL_HEADERS + [HEADER, CLEAR_HEADER]:
         with open(path, "rb") as f:
             h.update(f.read())
     h.update(" ".join(HIPCC_FLAGS).encode())

@@ -1,0 +1,97 @@
+// Argument checks and sizes of the clear track (include/ppmm.h).  No HIP here: the host tests compile this file alone.
+#ifndef PPMM_HOST_HPP
+#define PPMM_HOST_HPP
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/ppmm.h"
+
+namespace ppmm_host {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 24;        // M and T
+constexpr int64_t kMaxK = (int64_t)1 << 22;
+constexpr int64_t kMaxCodes = (int64_t)1 << 36;
+constexpr int64_t kMaxStride = (int64_t)1 << 40;      // elements; keeps every byte offset below 2^63
+
+inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// ---- 4-bit weights -------------------------------------------------------------------------------------------------
+
+inline pcmm_status check_weights(int64_t M, int64_t K, int32_t group, int32_t type, const void *codes, const void *scales, int32_t device)
+{
+    if (M <= 0 || K <= 0 || M > kMaxRows || K > kMaxK || device < 0 || !codes || !scales) return PCMM_EINVAL;
+    if (group != 32 && group != 64 && group != 128) return PCMM_EINVAL;
+    if (type != PPMM_BF16 && type != PPMM_FP16) return PCMM_EINVAL;
+    if (up(M, 16) * up(K, 128) > kMaxCodes) return PCMM_EUNSUPPORTED;
+    return PCMM_OK;
+}
+
+// *nothing: no tokens, a valid call without work
+inline pcmm_status check_product(int64_t M, int64_t K, int64_t T, const void *x, int64_t ldx, const void *y, int64_t ldy, bool *nothing)
+{
+    *nothing = false;
+    if (T < 0 || ldx < 0 || ldy < M) return PCMM_EINVAL;
+    if (T == 0) { *nothing = true; return PCMM_OK; }
+    if (!x || !y || x == y) return PCMM_EINVAL;
+    if (ldx != 0 && ldx < K) return PCMM_EINVAL;
+    if (T > kMaxRows || ldx > kMaxStride / T || ldy > kMaxStride / T) return PCMM_EUNSUPPORTED;
+    if ((up(M, 16) / 16) * (up(T, 64) / 64) > ((int64_t)1 << 24)) return PCMM_EUNSUPPORTED;
+    return PCMM_OK;
+}
+
+// ---- cache ---------------------------------------------------------------------------------------------------------
+
+inline bool geometry_ok(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim)
+{
+    return pages > 0 && pages <= 0x7fffffff && page_size > 0 && page_size <= 65536 && page_size % 16 == 0 && kv_heads > 0 &&
+           kv_heads <= 1024 && (head_dim == 64 || head_dim == 128);
+}
+
+// bytes of one page of one head: codes of keys and values, then (scale, offset) of keys and of values
+inline int64_t page_bytes(int32_t page_size, int32_t head_dim) { return (int64_t)page_size * (head_dim + head_dim / 4); }
+
+inline size_t pool_bytes(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim)
+{
+    if (!geometry_ok(pages, page_size, kv_heads, head_dim)) return 0;
+    const int64_t per_page = page_bytes(page_size, head_dim) * kv_heads;
+    if (pages >= (((int64_t)1 << 47) + per_page - 1) / per_page) return 0;
+    return (size_t)(pages * per_page);
+}
+
+inline pcmm_status check_cache(const ppkv_cache *c, const ppkv_batch *b, int64_t tokens, int32_t device)
+{
+    if (!c || !b || device < 0 || tokens < 0 || tokens > 0x7fffffff) return PCMM_EINVAL;
+    if (!c->pool || ((uintptr_t)c->pool & 15) || pool_bytes(c->pages, c->page_size, c->kv_heads, c->head_dim) == 0) return PCMM_EINVAL;
+    if (!b->starts || !b->lens || !b->table || b->batch <= 0 || b->batch > 65535 || b->table_width <= 0) return PCMM_EINVAL;
+    if ((int64_t)b->table_width * c->page_size > 0x7fffffff) return PCMM_EINVAL;
+    return PCMM_OK;
+}
+
+inline bool read_strides_ok(int64_t token_stride, int64_t head_stride)
+{
+    return token_stride >= 0 && head_stride >= 0 && token_stride <= kMaxStride / 0x7fffffff * 1024 && head_stride <= kMaxStride;
+}
+
+// no two of tokens x heads rows of D elements overlap
+inline bool rows_apart(int64_t tokens, int64_t heads, int64_t D, int64_t token_stride, int64_t head_stride)
+{
+    if (!read_strides_ok(token_stride, head_stride)) return false;
+    const bool token_inner = heads == 1 || (tokens > 0 && head_stride >= (tokens - 1) * token_stride + D);
+    const bool head_inner = tokens <= 1 || token_stride >= (heads - 1) * head_stride + D;
+    return (head_inner && (heads == 1 || head_stride >= D)) || (token_inner && (tokens <= 1 || token_stride >= D));
+}
+
+inline pcmm_status check_attention(const ppkv_cache *c, const ppkv_batch *b, int64_t tokens, int32_t type, int32_t heads, int32_t max_q,
+                                   int64_t max_len, int32_t device)
+{
+    const pcmm_status rc = check_cache(c, b, tokens, device);
+    if (rc != PCMM_OK) return rc;
+    if ((type != PPMM_BF16 && type != PPMM_FP16) || max_q < 0 || max_len < 0) return PCMM_EINVAL;
+    if (heads <= 0 || heads % c->kv_heads != 0 || heads / c->kv_heads > 65536) return PCMM_EINVAL;
+    return PCMM_OK;
+}
+
+}  // namespace ppmm_host
+
+#endif  // PPMM_HOST_HPP
