@@ -9,8 +9,47 @@
 
 namespace ppmm {
 
-struct BF16 { using type = __bf16; };
-struct FP16 { using type = _Float16; };
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// The two 16-bit types.  kSixteen: the bits of 16.0; a 4-bit code in the top four mantissa bits, at kCodeBit, makes it 16 + code
+// exactly.  kMinus24: the bits of -24.0 = -(16 + 8), twice.  mma: D = A B + C on a 16 x 16 tile with 32 values of k: lane l holds
+// row (A) or column (B) l % 16 and k = 8 (l / 16) ... + 7, of C and D column l % 16 and rows 4 (l / 16) ... + 3.
+struct BF16 {
+    using type = __bf16;
+    static constexpr int kCodeBit = 3;
+    static constexpr uint32_t kSixteen = 0x41804180u, kMinus24 = 0xC1C0C1C0u;
+    static __device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct FP16 {
+    using type = _Float16;
+    static constexpr int kCodeBit = 6;
+    static constexpr uint32_t kSixteen = 0x4C004C00u, kMinus24 = 0xCE00CE00u;
+    static __device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+__device__ inline uint32_t rotate_right(uint32_t v, int by) { return __builtin_amdgcn_alignbit(v, v, by); }
+
+// Eight codes -> eight values 16 + code.  Of the word's nibbles, counted from bit kCodeBit on and around the end, number i and
+// number 4 + i become the pair i: a rotation and a mask-and-or each.
+template <class T> __device__ inline u32x4 unpack(uint32_t w)
+{
+    constexpr uint32_t mask = 0x000F000Fu << T::kCodeBit;
+    u32x4 v;
+    v[0] = (w & mask) | T::kSixteen;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) v[i] = (rotate_right(w, 4 * i) & mask) | T::kSixteen;
+    return v;
+}
 
 template <class T> __device__ inline float to_f32(uint16_t bits) { return (float)__builtin_bit_cast(typename T::type, bits); }
 template <class T> __device__ inline uint16_t from_f32(float v) { return __builtin_bit_cast(uint16_t, (typename T::type)v); }   // to nearest even

@@ -1,5 +1,15 @@
 // Products with weights held in 4 bits under group scales (include/ppmm.h; Section 5.1's linear layers for clear tokens), on
 // MI355X (gfx950).
+//
+//     y[t][m] = sum_g s[m][g] sum_{k in g} (c[m][k] - 8) x[t][k]  +  sum_g o[m][g] sum_{k in g} x[t][k]
+//
+// A code never becomes a scaled 16-bit weight, which would round it: the matrix cores multiply x with 16 + c, which a 16-bit
+// float holds exactly and which one mask-and-or makes of a code, and with -24 = -(16 + 8) in the same chain; the 32-bit sum over
+// a group is then scaled.  The chain of -24 x also is the group's sum of x that the offsets need.
+//
+// Layout of a plan.  Blocks of 16 rows x 128 k, 1 KiB, in the order of the matrix instruction's operand: lane l has row l % 16
+// and 16 bytes, word j of it k = 32 j + 8 (l / 16) ... + 7.  A wave fetches a block with one 16-byte load per lane, and a
+// work-group's waves read neighbouring blocks.  Scales (and offsets) of a group: 16 rows side by side.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -13,50 +23,206 @@ struct ppmv_plan {
     int64_t M, K;
     int32_t group, type, device;
     bool has_offsets;
-    uint8_t *codes;
-    uint16_t *scales, *offsets;
+    uint32_t *codes;     // [ceil(M/16)][ceil(K/128)][64 lanes][4 words]
+    uint16_t *params;    // [ceil(M/16)][ceil(K/128) * 128/group][scales, offsets if any][16 rows]
     size_t bytes;
 };
 
 namespace {
 
 using ppmm::BF16;
+using ppmm::f32x4;
 using ppmm::FP16;
+using ppmm::u32x2;
+using ppmm::u32x4;
 
 struct Weights {
-    const uint8_t *codes;
-    const uint16_t *scales, *offsets;
+    const u32x4 *codes;
+    const uint16_t *params;
 };
 
-template <class T>
-__device__ inline float dot(const Weights &w, const uint16_t *x, int64_t m, int64_t K, int32_t group)
+// ---- packing -------------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t *codes, uint32_t *out, int64_t M, int64_t K, int64_t kblocks, int64_t first, int64_t words,
+                                                         int code_bit)
 {
-    const int64_t groups = (K + group - 1) / group, half = (K + 1) / 2;
-    float sum = 0.0f;
-    for (int64_t k = threadIdx.x; k < K; k += 64) {
-        const int c = w.codes[m * half + k / 2] >> (4 * (k & 1)) & 15;
-        const float s = ppmm::to_f32<T>(w.scales[m * groups + k / group]);
-        const float o = w.offsets ? ppmm::to_f32<T>(w.offsets[m * groups + k / group]) : 0.0f;
-        sum = fmaf(ppmm::to_f32<T>(x[k]), fmaf(s, (float)(c - 8), o), sum);
-    }
-    for (int step = 32; step; step /= 2) sum += __shfl_xor(sum, step);
-    return sum;
+    const int64_t idx = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= first + words) return;
+    const int j = (int)(idx % 4), lane = (int)(idx / 4 % 64);
+    const int64_t block = idx / 256, m = block / kblocks * 16 + lane % 16, k = block % kblocks * 128 + 32 * j + 8 * (lane / 16);
+    const int64_t half = (K + 1) / 2;
+    uint32_t w = 0;
+    if (m < M)
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = k / 2 + i;
+            const uint32_t pair = at < half ? codes[m * half + at] : 0;
+            w |= (pair & 15) << (4 * i) | (pair >> 4) << (16 + 4 * i);
+        }
+    out[idx] = w << code_bit | w >> (32 - code_bit);
 }
 
-// One wave a result.
-template <class T, bool kGated>
-__global__ __launch_bounds__(64) void product_kernel(Weights a, Weights b, int64_t M, int64_t K, int32_t group, int64_t T_, const uint16_t *x,
-                                                     int64_t ldx, uint16_t *y, int64_t ldy)
+__global__ __launch_bounds__(256) void pack_params_kernel(const uint16_t *scales, const uint16_t *offsets, uint16_t *out, int64_t M, int64_t groups,
+                                                          int64_t groups_up, int64_t first, int64_t count)
 {
-    const int64_t m = blockIdx.x;
-    for (int64_t t = blockIdx.y; t < T_; t += gridDim.y) {
-        float r = dot<T>(a, x + t * ldx, m, K, group);
-        if (kGated) {
-            const float u = dot<T>(b, x + t * ldx, m, K, group);
-            r = r / (1.0f + expf(-r)) * u;
-        }
-        if (threadIdx.x == 0) y[t * ldy + m] = ppmm::from_f32<T>(r);
+    const int64_t idx = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= first + count) return;
+    const int kinds = offsets ? 2 : 1;
+    const int64_t row = idx % 16, kind = idx / 16 % kinds, g = idx / 16 / kinds % groups_up, m = idx / 16 / kinds / groups_up * 16 + row;
+    out[idx] = m < M && g < groups ? (kind ? offsets : scales)[m * groups + g] : 0;
+}
+
+// ---- a few tokens --------------------------------------------------------------------------------------------------
+// HBM-bound: the weights stream through once and every token rides along.  A work-group of eight waves takes kRows tiles of 16
+// rows (of both matrices, if gated) and kTok tiles of 16 tokens; its waves share out the blocks of K and add up through LDS.
+constexpr int kWaves = 8;
+
+// eight values of one token from k on, zero behind K
+__device__ inline u32x4 load_x(const uint16_t *row, int64_t k, int64_t K, bool aligned)
+{
+    u32x4 v = {0, 0, 0, 0};
+    if (aligned && k + 8 <= K) return *(const u32x4 *)(row + k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k + i < K) v[i / 2] |= (uint32_t)row[k + i] << (16 * (i % 2));
+    return v;
+}
+
+template <class T> __device__ inline f32x4 four(u32x2 v)
+{
+    return f32x4{ppmm::to_f32<T>((uint16_t)v[0]), ppmm::to_f32<T>((uint16_t)(v[0] >> 16)), ppmm::to_f32<T>((uint16_t)v[1]), ppmm::to_f32<T>((uint16_t)(v[1] >> 16))};
+}
+
+__device__ inline float silu_times(float g, float u)
+{
+    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)) * u;
+}
+
+template <class T, int kTok, int kRows, int kGroups, bool kGated>
+__global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, bool offsets, int64_t M, int64_t K, int kblocks, int64_t tokens,
+                                                                 const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+{
+    constexpr int kMats = kGated ? 2 : 1;
+    constexpr int kSteps = 4 / kGroups;             // matrix instructions of a group
+    __shared__ f32x4 part[kWaves][kMats * kRows][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
+    const int64_t tiles = (M + 15) / 16, tile0 = (int64_t)blockIdx.x * kRows, t0 = (int64_t)blockIdx.y * 16 * kTok;
+    const int kinds = offsets ? 2 : 1;
+    f32x4 sum[kMats][kRows][kTok] = {};
+    int64_t tile[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) tile[r] = tile0 + r < tiles ? tile0 + r : tiles - 1;
+    const uint16_t *row[kTok];
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) row[t] = x + (t0 + 16 * t + col) * ldx;
+    const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
+    for (int kb = wave; kb < kblocks; kb += kWaves) {
+        u32x4 codes[kMats][kRows], xs[kTok][4];
+        u32x2 s[kMats][kRows][kGroups], o[kMats][kRows][kGroups] = {};
+#pragma unroll
+        for (int w = 0; w < kMats; ++w)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const Weights &m = w ? b : a;
+                codes[w][r] = m.codes[(tile[r] * kblocks + kb) * 64 + lane];
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const uint16_t *p = m.params + ((tile[r] * kblocks + kb) * kGroups + g) * kinds * 16 + 4 * h;
+                    s[w][r][g] = *(const u32x2 *)p;
+                    if (offsets) o[w][r][g] = *(const u32x2 *)(p + 16);
+                }
+            }
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                xs[t][j] = u32x4{0, 0, 0, 0};
+                if (t0 + 16 * t + col < tokens) xs[t][j] = load_x(row[t], (int64_t)kb * 128 + 32 * j + 8 * h, K, aligned);
+            }
+        f32x4 base[kTok][kGroups];                  // -24 times the group's sum of x, in every row
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                base[t][j / kSteps] = T::mma(minus24, xs[t][j], j % kSteps ? base[t][j / kSteps] : f32x4{0, 0, 0, 0});
+#pragma unroll
+        for (int w = 0; w < kMats; ++w)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    f32x4 acc[kTok];
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) {
+                        const u32x4 v = ppmm::unpack<T>(codes[w][r][g * kSteps + j]);
+#pragma unroll
+                        for (int t = 0; t < kTok; ++t) acc[t] = T::mma(v, xs[t][g * kSteps + j], j ? acc[t] : base[t][g]);
+                    }
+                    const f32x4 sf = four<T>(s[w][r][g]), of = four<T>(o[w][r][g]) * (-1.0f / 24.0f);
+#pragma unroll
+                    for (int t = 0; t < kTok; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sum[w][r][t][i] = fmaf(sf[i], acc[t][i], sum[w][r][t][i]);
+                            if (offsets) sum[w][r][t][i] = fmaf(of[i], base[t][g][i], sum[w][r][t][i]);
+                        }
+                }
     }
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kMats; ++w)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) part[wave][w * kRows + r][lane] = sum[w][r][t];
+        __syncthreads();
+        // a thread finishes one result of every tile it takes: 16 x 16 results of kRows tiles
+        for (int i = threadIdx.x; i < kRows * 256; i += 64 * kWaves) {
+            const int r = i / 256, e = i % 4, l = i / 4 % 64;
+            float v[kMats];
+#pragma unroll
+            for (int w = 0; w < kMats; ++w) {
+                v[w] = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kWaves; ++q) v[w] += part[q][w * kRows + r][l][e];
+            }
+            const int64_t m = (tile0 + r) * 16 + 4 * (l / 16) + e, n = t0 + 16 * t + l % 16;
+            if (m < M && n < tokens) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0], v[kMats - 1]) : v[0]);
+        }
+    }
+}
+
+struct Call {
+    const ppmv_plan *p, *u;
+    int64_t T;
+    const uint16_t *x;
+    int64_t ldx;
+    uint16_t *y;
+    int64_t ldy;
+    hipStream_t stream;
+};
+
+template <class T, int kTok, int kRows, int kGroups, bool kGated> void launch_few(const Call &c)
+{
+    const ppmv_plan *p = c.p, *u = c.u;
+    const int64_t tiles = (p->M + 15) / 16;
+    const dim3 grid((unsigned)((tiles + kRows - 1) / kRows), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
+    const bool aligned = ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0;
+    const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
+    hipLaunchKernelGGL((few_tokens_kernel<T, kTok, kRows, kGroups, kGated>), grid, dim3(64 * kWaves), 0, c.stream, a, b, p->has_offsets, p->M, p->K,
+                       (int)((p->K + 127) / 128), c.T, c.x, c.ldx, aligned, c.y, c.ldy);
+}
+
+template <class T, int kGroups, bool kGated> void launch(const Call &c)
+{
+    if (c.T <= 16) launch_few<T, 1, 1, kGroups, kGated>(c);
+    else if (c.T <= 32) launch_few<T, 2, 2, kGroups, kGated>(c);
+    else launch_few<T, 4, 2, kGroups, kGated>(c);
+}
+
+template <class T, bool kGated> void by_group(const Call &c)
+{
+    if (c.p->group == 128) launch<T, 1, kGated>(c);
+    else if (c.p->group == 64) launch<T, 2, kGated>(c);
+    else launch<T, 4, kGated>(c);
 }
 
 template <bool kGated>
@@ -67,10 +233,9 @@ pcmm_status run(const ppmv_plan *p, const ppmv_plan *u, int64_t T, const void *x
     if (rc != PCMM_OK || nothing) return rc;
     pcmm_hip_util::DevGuard dg(p->device);
     if (!dg.ok) return PCMM_EDEVICE;
-    auto kernel = p->type == PPMM_BF16 ? product_kernel<BF16, kGated> : product_kernel<FP16, kGated>;
-    const Weights a{p->codes, p->scales, p->offsets}, b{u->codes, u->scales, u->offsets};
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p->M, (unsigned)(T < 128 ? T : 128)), dim3(64), 0, (hipStream_t)stream, a, b, p->M, p->K, p->group, T,
-                       (const uint16_t *)x, ldx, (uint16_t *)y, ldy);
+    const Call c{p, u, T, (const uint16_t *)x, ldx, (uint16_t *)y, ldy, (hipStream_t)stream};
+    if (p->type == PPMM_BF16) by_group<BF16, kGated>(c);
+    else by_group<FP16, kGated>(c);
     return hipGetLastError() == hipSuccess ? PCMM_OK : PCMM_EDEVICE;
 }
 
@@ -91,20 +256,29 @@ pcmm_status ppmv_plan_create(ppmv_plan **out, int64_t M, int64_t K, int32_t grou
     pcmm_hip_util::DevGuard dg(device);
     if (!dg.ok) { delete p; return PCMM_EDEVICE; }
     hipStream_t st = (hipStream_t)stream;
-    const size_t code_bytes = (size_t)M * ((K + 1) / 2), param_bytes = (size_t)M * ((K + group - 1) / group) * 2;
+    const int64_t tiles = (M + 15) / 16, kblocks = (K + 127) / 128, words = tiles * kblocks * 256;
+    const int64_t groups_up = kblocks * (128 / group), count = tiles * groups_up * (offsets_dev ? 32 : 16);
     pcmm_status rc = PCMM_OK;
-    if (hipMalloc((void **)&p->codes, code_bytes) != hipSuccess || hipMalloc((void **)&p->scales, param_bytes) != hipSuccess ||
-        (offsets_dev && hipMalloc((void **)&p->offsets, param_bytes) != hipSuccess)) {
+    if (hipMalloc((void **)&p->codes, (size_t)words * 4) != hipSuccess || hipMalloc((void **)&p->params, (size_t)count * 2) != hipSuccess) {
         (void)hipGetLastError();
         rc = PCMM_ENOMEM;
     }
-    p->bytes = code_bytes + param_bytes * (offsets_dev ? 2 : 1);
-    if (rc == PCMM_OK &&
-        (hipMemcpyAsync(p->codes, codes_dev, code_bytes, hipMemcpyDeviceToDevice, st) != hipSuccess ||
-         hipMemcpyAsync(p->scales, scales_dev, param_bytes, hipMemcpyDeviceToDevice, st) != hipSuccess ||
-         (offsets_dev && hipMemcpyAsync(p->offsets, offsets_dev, param_bytes, hipMemcpyDeviceToDevice, st) != hipSuccess) ||
-         hipStreamSynchronize(st) != hipSuccess))
-        rc = PCMM_EDEVICE;
+    p->bytes = (size_t)words * 4 + (size_t)count * 2;
+    if (rc == PCMM_OK) {
+        // check_weights holds words to 2^33; no launch has 2^32 threads or more
+        const int64_t most = (int64_t)1 << 31;
+        for (int64_t at = 0; at < words; at += most) {
+            const int64_t n = words - at < most ? words - at : most;
+            hipLaunchKernelGGL(pack_codes_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, codes_dev, p->codes, M, K, kblocks, at, n,
+                               type == PPMM_BF16 ? BF16::kCodeBit : FP16::kCodeBit);
+        }
+        for (int64_t at = 0; at < count; at += most) {
+            const int64_t n = count - at < most ? count - at : most;
+            hipLaunchKernelGGL(pack_params_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const uint16_t *)scales_dev,
+                               (const uint16_t *)offsets_dev, p->params, M, (K + group - 1) / group, groups_up, at, n);
+        }
+        if (hipGetLastError() != hipSuccess || hipStreamSynchronize(st) != hipSuccess) rc = PCMM_EDEVICE;
+    }
     if (rc != PCMM_OK) { ppmv_plan_destroy(p); return rc; }
     *out = p;
     return PCMM_OK;
@@ -133,8 +307,7 @@ void ppmv_plan_destroy(ppmv_plan *plan)
     if (!plan) return;
     pcmm_hip_util::DevGuard dg(plan->device);
     (void)hipFree(plan->codes);
-    (void)hipFree(plan->scales);
-    (void)hipFree(plan->offsets);
+    (void)hipFree(plan->params);
     delete plan;
 }
 
