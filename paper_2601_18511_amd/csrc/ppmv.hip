@@ -9,7 +9,8 @@
 //
 // Layout of a plan.  Blocks of 16 rows x 128 k, 1 KiB, in the order of the matrix instruction's operand: lane l has row l % 16
 // and 16 bytes, word j of it k = 32 j + 8 (l / 16) ... + 7.  A wave fetches a block with one 16-byte load per lane, and a
-// work-group's waves read neighbouring blocks.  Scales (and offsets) of a group: 16 rows side by side.
+// work-group's waves read neighbouring blocks.  What a lane needs of a block's scales (and offsets), its four rows of every group,
+// lies side by side: 8 to 64 bytes.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,7 +25,7 @@ struct ppmv_plan {
     int32_t group, type, device;
     bool has_offsets;
     uint32_t *codes;     // [ceil(M/16)][ceil(K/128)][64 lanes][4 words]
-    uint16_t *params;    // [ceil(M/16)][ceil(K/128) * 128/group][scales, offsets if any][16 rows]
+    uint16_t *params;    // [ceil(M/16)][ceil(K/128)][4 quarters][128/group][scales, offsets if any][4 rows of the quarter]
     size_t bytes;
 };
 
@@ -61,19 +62,19 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t *codes, u
 }
 
 __global__ __launch_bounds__(256) void pack_params_kernel(const uint16_t *scales, const uint16_t *offsets, uint16_t *out, int64_t M, int64_t groups,
-                                                          int64_t groups_up, int64_t first, int64_t count)
+                                                          int64_t kblocks, int per_block, int64_t first, int64_t count)
 {
     const int64_t idx = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= first + count) return;
     const int kinds = offsets ? 2 : 1;
-    const int64_t row = idx % 16, kind = idx / 16 % kinds, g = idx / 16 / kinds % groups_up, m = idx / 16 / kinds / groups_up * 16 + row;
+    const int64_t row = idx % 4, kind = idx / 4 % kinds, in_block = idx / 4 / kinds % per_block, rest = idx / 4 / kinds / per_block;
+    const int64_t quarter = rest % 4, kb = rest / 4 % kblocks, m = rest / 4 / kblocks * 16 + 4 * quarter + row, g = kb * per_block + in_block;
     out[idx] = m < M && g < groups ? (kind ? offsets : scales)[m * groups + g] : 0;
 }
 
 // ---- a few tokens --------------------------------------------------------------------------------------------------
-// HBM-bound: the weights stream through once and every token rides along.  A work-group of eight waves takes kRows tiles of 16
+// HBM-bound: the weights stream through once and every token rides along.  A work-group of kWaves waves takes kRows tiles of 16
 // rows (of both matrices, if gated) and kTok tiles of 16 tokens; its waves share out the blocks of K and add up through LDS.
-constexpr int kWaves = 8;
 
 // eight values of one token from k on, zero behind K
 __device__ inline u32x4 load_x(const uint16_t *row, int64_t k, int64_t K, bool aligned)
@@ -96,40 +97,161 @@ __device__ inline float silu_times(float g, float u)
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)) * u;
 }
 
-template <class T, int kTok, int kRows, int kGroups, bool kGated>
-__global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, bool offsets, int64_t M, int64_t K, int kblocks, int64_t tokens,
-                                                                 const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+// Scales and offsets of one block: kGroups groups of the lane's four rows.
+template <int kGroups, bool kOffsets> struct Params {
+    static constexpr int kKinds = kOffsets ? 2 : 1, kStride = kGroups * kKinds * 16;      // 16-bit words of a block
+    u32x2 v[kGroups * kKinds];
+    __device__ inline void load(const uint16_t *block, int h)
+    {
+        const uint16_t *p = block + h * kGroups * kKinds * 4;
+        if constexpr (kGroups * kKinds == 1) v[0] = *(const u32x2 *)p;
+        else
+#pragma unroll
+            for (int i = 0; i < kGroups * kKinds; i += 2) {
+                const u32x4 w = *(const u32x4 *)(p + 4 * i);
+                v[i] = u32x2{w[0], w[1]};
+                v[i + 1] = u32x2{w[2], w[3]};
+            }
+    }
+};
+
+// -24 times the sum of x over each group of a block, in every row of the tile
+template <class T, int kGroups> __device__ inline void group_sums(f32x4 (&base)[kGroups], const u32x4 (&x)[4])
+{
+    constexpr int kSteps = 4 / kGroups;
+    const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) base[j / kSteps] = T::mma(minus24, x[j], j % kSteps ? base[j / kSteps] : f32x4{0, 0, 0, 0});
+}
+
+// sum += block times the kTok tiles of x
+template <class T, int kTok, int kGroups, bool kOffsets>
+__device__ inline void add_block(f32x4 (&sum)[kTok], u32x4 codes, const Params<kGroups, kOffsets> &p, const u32x4 (&x)[kTok][4],
+                                 const f32x4 (&base)[kTok][kGroups])
+{
+    constexpr int kSteps = 4 / kGroups, kKinds = kOffsets ? 2 : 1;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        f32x4 acc[kTok];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const u32x4 v = ppmm::unpack<T>(codes[g * kSteps + j]);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) acc[t] = T::mma(v, x[t][g * kSteps + j], j ? acc[t] : base[t][g]);
+        }
+        const f32x4 s = four<T>(p.v[g * kKinds]);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(s[e], acc[t][e], sum[t][e]);
+        if constexpr (kOffsets) {
+            const f32x4 o = four<T>(p.v[g * kKinds + 1]) * (-1.0f / 24.0f);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(o[e], base[t][g][e], sum[t][e]);
+        }
+    }
+}
+
+// Adds up what the waves left in part and stores 16 tokens from t0 on, 16 rows of kRows tiles; a thread finishes one result of each
+// tile it takes.
+template <class T, int kRows, int kWaves, bool kGated>
+__device__ inline void finish(const f32x4 (&part)[kWaves][kRows * (kGated ? 2 : 1)][64], int64_t tile0, int64_t t0, int64_t M, int64_t tokens, uint16_t *y,
+                              int64_t ldy)
 {
     constexpr int kMats = kGated ? 2 : 1;
-    constexpr int kSteps = 4 / kGroups;             // matrix instructions of a group
-    __shared__ f32x4 part[kWaves][kMats * kRows][64];
+    for (int i = threadIdx.x; i < kRows * 256; i += 64 * kWaves) {
+        const int r = i / 256, e = i % 4, l = i / 4 % 64;
+        float v[kMats];
+#pragma unroll
+        for (int w = 0; w < kMats; ++w) {
+            v[w] = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kWaves; ++q) v[w] += part[q][w * kRows + r][l][e];
+        }
+        const int64_t m = (tile0 + r) * 16 + 4 * (l / 16) + e, n = t0 + l % 16;
+        if (m < M && n < tokens) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0], v[kMats - 1]) : v[0]);
+    }
+}
+
+// Up to four tokens whose rows fit LDS together.  Columns without a token carry the last one's values and are not stored.  With x
+// out of the way nothing but weights is in the queue of loads, and a wave asks for its next block before it uses the present one;
+// more blocks ahead (2 or 4) took registers and with them waves: 14336 x 4096 gated, group 64, 14.6 and 15.5 us for 14.0.
+template <class T, int kWaves, int kGroups, bool kGated, bool kOffsets>
+__global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights b, int64_t M, int K, int kblocks, int tokens, const uint16_t *x,
+                                                             int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+{
+    constexpr int kMats = kGated ? 2 : 1;
+    using Par = Params<kGroups, kOffsets>;
+    extern __shared__ u32x4 rows[];                 // [tokens][kblocks * 16 + 1]
+    __shared__ f32x4 part[kWaves][kMats][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
+    const int64_t tile = blockIdx.x;
+    u32x4 codes[kMats];
+    Par params[kMats];
+    const auto fetch = [&](int kb) {
+#pragma unroll
+        for (int w = 0; w < kMats; ++w) {
+            const Weights &m = w ? b : a;
+            codes[w] = m.codes[(tile * kblocks + kb) * 64 + lane];
+            params[w].load(m.params + (tile * kblocks + kb) * Par::kStride, h);
+        }
+    };
+    if (wave < kblocks) fetch(wave);
+    const int pitch = kblocks * 16 + 1;             // the odd one keeps the rows on different banks
+    for (int t = 0; t < tokens; ++t)
+        for (int i = threadIdx.x; i < kblocks * 16; i += 64 * kWaves) rows[t * pitch + i] = load_x(x + t * ldx, 8 * i, K, aligned);
+    __syncthreads();
+    const u32x4 *mine = rows + (col < tokens ? col : tokens - 1) * pitch + h;
+    f32x4 sum[kMats][1] = {};
+    for (int kb = wave; kb < kblocks; kb += kWaves) {
+        u32x4 xs[1][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xs[0][j] = mine[kb * 16 + 4 * j];
+        f32x4 base[1][kGroups];
+        group_sums<T, kGroups>(base[0], xs[0]);
+#pragma unroll
+        for (int w = 0; w < kMats; ++w) add_block<T, 1, kGroups, kOffsets>(sum[w], codes[w], params[w], xs, base);
+        if (kb + kWaves < kblocks) fetch(kb + kWaves);
+    }
+#pragma unroll
+    for (int w = 0; w < kMats; ++w) part[wave][w][lane] = sum[w][0];
+    __syncthreads();
+    finish<T, 1, kWaves, kGated>(part, tile, 0, M, tokens, y, ldy);
+}
+
+// Any number of tokens; x comes from the caches as the matrix instruction wants it.
+template <class T, int kTok, int kRows, int kWaves, int kGroups, bool kGated, bool kOffsets>
+__global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens,
+                                                                 const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+{
+    constexpr int kTiles = kRows * (kGated ? 2 : 1);
+    using Par = Params<kGroups, kOffsets>;
+    __shared__ f32x4 part[kWaves][kTiles][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
     const int64_t tiles = (M + 15) / 16, tile0 = (int64_t)blockIdx.x * kRows, t0 = (int64_t)blockIdx.y * 16 * kTok;
-    const int kinds = offsets ? 2 : 1;
-    f32x4 sum[kMats][kRows][kTok] = {};
-    int64_t tile[kRows];
+    f32x4 sum[kTiles][kTok] = {};
+    const u32x4 *codes_of[kTiles];
+    const uint16_t *params_of[kTiles];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) tile[r] = tile0 + r < tiles ? tile0 + r : tiles - 1;
+    for (int i = 0; i < kTiles; ++i) {              // a tile behind the last one is the last one once more
+        const Weights &w = i / kRows ? b : a;
+        const int64_t tile = tile0 + i % kRows < tiles ? tile0 + i % kRows : tiles - 1;
+        codes_of[i] = w.codes + tile * kblocks * 64 + lane;
+        params_of[i] = w.params + tile * kblocks * Par::kStride;
+    }
     const uint16_t *row[kTok];
 #pragma unroll
     for (int t = 0; t < kTok; ++t) row[t] = x + (t0 + 16 * t + col) * ldx;
-    const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
     for (int kb = wave; kb < kblocks; kb += kWaves) {
-        u32x4 codes[kMats][kRows], xs[kTok][4];
-        u32x2 s[kMats][kRows][kGroups], o[kMats][kRows][kGroups] = {};
+        u32x4 codes[kTiles], xs[kTok][4];
+        Par params[kTiles];
 #pragma unroll
-        for (int w = 0; w < kMats; ++w)
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const Weights &m = w ? b : a;
-                codes[w][r] = m.codes[(tile[r] * kblocks + kb) * 64 + lane];
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    const uint16_t *p = m.params + ((tile[r] * kblocks + kb) * kGroups + g) * kinds * 16 + 4 * h;
-                    s[w][r][g] = *(const u32x2 *)p;
-                    if (offsets) o[w][r][g] = *(const u32x2 *)(p + 16);
-                }
-            }
+        for (int i = 0; i < kTiles; ++i) {
+            codes[i] = codes_of[i][(int64_t)kb * 64];
+            params[i].load(params_of[i] + (int64_t)kb * Par::kStride, h);
+        }
 #pragma unroll
         for (int t = 0; t < kTok; ++t)
 #pragma unroll
@@ -137,56 +259,19 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
                 xs[t][j] = u32x4{0, 0, 0, 0};
                 if (t0 + 16 * t + col < tokens) xs[t][j] = load_x(row[t], (int64_t)kb * 128 + 32 * j + 8 * h, K, aligned);
             }
-        f32x4 base[kTok][kGroups];                  // -24 times the group's sum of x, in every row
+        f32x4 base[kTok][kGroups];
 #pragma unroll
-        for (int t = 0; t < kTok; ++t)
+        for (int t = 0; t < kTok; ++t) group_sums<T, kGroups>(base[t], xs[t]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                base[t][j / kSteps] = T::mma(minus24, xs[t][j], j % kSteps ? base[t][j / kSteps] : f32x4{0, 0, 0, 0});
-#pragma unroll
-        for (int w = 0; w < kMats; ++w)
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    f32x4 acc[kTok];
-#pragma unroll
-                    for (int j = 0; j < kSteps; ++j) {
-                        const u32x4 v = ppmm::unpack<T>(codes[w][r][g * kSteps + j]);
-#pragma unroll
-                        for (int t = 0; t < kTok; ++t) acc[t] = T::mma(v, xs[t][g * kSteps + j], j ? acc[t] : base[t][g]);
-                    }
-                    const f32x4 sf = four<T>(s[w][r][g]), of = four<T>(o[w][r][g]) * (-1.0f / 24.0f);
-#pragma unroll
-                    for (int t = 0; t < kTok; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            sum[w][r][t][i] = fmaf(sf[i], acc[t][i], sum[w][r][t][i]);
-                            if (offsets) sum[w][r][t][i] = fmaf(of[i], base[t][g][i], sum[w][r][t][i]);
-                        }
-                }
+        for (int i = 0; i < kTiles; ++i) add_block<T, kTok, kGroups, kOffsets>(sum[i], codes[i], params[i], xs, base);
     }
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
+        if (t) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) part[wave][i][lane] = sum[i][t];
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kMats; ++w)
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) part[wave][w * kRows + r][lane] = sum[w][r][t];
-        __syncthreads();
-        // a thread finishes one result of every tile it takes: 16 x 16 results of kRows tiles
-        for (int i = threadIdx.x; i < kRows * 256; i += 64 * kWaves) {
-            const int r = i / 256, e = i % 4, l = i / 4 % 64;
-            float v[kMats];
-#pragma unroll
-            for (int w = 0; w < kMats; ++w) {
-                v[w] = 0.0f;
-#pragma unroll
-                for (int q = 0; q < kWaves; ++q) v[w] += part[q][w * kRows + r][l][e];
-            }
-            const int64_t m = (tile0 + r) * 16 + 4 * (l / 16) + e, n = t0 + 16 * t + l % 16;
-            if (m < M && n < tokens) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0], v[kMats - 1]) : v[0]);
-        }
+        finish<T, kRows, kWaves, kGated>(part, tile0, t0 + 16 * t, M, tokens, y, ldy);
     }
 }
 
@@ -200,20 +285,38 @@ struct Call {
     hipStream_t stream;
 };
 
+bool aligned16(const Call &c) { return ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0; }
+
 template <class T, int kTok, int kRows, int kGroups, bool kGated> void launch_few(const Call &c)
 {
     const ppmv_plan *p = c.p, *u = c.u;
     const int64_t tiles = (p->M + 15) / 16;
     const dim3 grid((unsigned)((tiles + kRows - 1) / kRows), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
-    const bool aligned = ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0;
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
-    hipLaunchKernelGGL((few_tokens_kernel<T, kTok, kRows, kGroups, kGated>), grid, dim3(64 * kWaves), 0, c.stream, a, b, p->has_offsets, p->M, p->K,
-                       (int)((p->K + 127) / 128), c.T, c.x, c.ldx, aligned, c.y, c.ldy);
+    auto kernel = p->has_offsets ? few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, true> : few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, aligned16(c), c.y, c.ldy);
+}
+
+template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(const Call &c)
+{
+    const ppmv_plan *p = c.p, *u = c.u;
+    const int kblocks = (int)((p->K + 127) / 128);
+    const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
+    auto kernel = p->has_offsets ? stream_kernel<T, kWaves, kGroups, kGated, true> : stream_kernel<T, kWaves, kGroups, kGated, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p->M + 15) / 16)), dim3(64 * kWaves), (size_t)c.T * (kblocks * 16 + 1) * 16, c.stream, a, b, p->M, (int)p->K,
+                       kblocks, (int)c.T, c.x, c.ldx, aligned16(c), c.y, c.ldy);
 }
 
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
 {
-    if (c.T <= 16) launch_few<T, 1, 1, kGroups, kGated>(c);
+    if (c.T <= 4 && c.T * c.p->K <= 16384) {
+        // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
+        // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.  (Two matrices in groups of 32 do not fit the registers then.)
+        if constexpr (!(kGated && kGroups == 4)) {
+            if (c.p->M <= 8192 && c.p->K > 8192) return launch_stream<T, 16, kGroups, kGated>(c);
+        }
+        launch_stream<T, 8, kGroups, kGated>(c);
+    } else if (c.T <= 16) launch_few<T, 1, 1, kGroups, kGated>(c);
     else if (c.T <= 32) launch_few<T, 2, 2, kGroups, kGated>(c);
     else launch_few<T, 4, 2, kGroups, kGated>(c);
 }
@@ -257,7 +360,7 @@ pcmm_status ppmv_plan_create(ppmv_plan **out, int64_t M, int64_t K, int32_t grou
     if (!dg.ok) { delete p; return PCMM_EDEVICE; }
     hipStream_t st = (hipStream_t)stream;
     const int64_t tiles = (M + 15) / 16, kblocks = (K + 127) / 128, words = tiles * kblocks * 256;
-    const int64_t groups_up = kblocks * (128 / group), count = tiles * groups_up * (offsets_dev ? 32 : 16);
+    const int64_t count = tiles * kblocks * (128 / group) * (offsets_dev ? 32 : 16);
     pcmm_status rc = PCMM_OK;
     if (hipMalloc((void **)&p->codes, (size_t)words * 4) != hipSuccess || hipMalloc((void **)&p->params, (size_t)count * 2) != hipSuccess) {
         (void)hipGetLastError();
@@ -275,7 +378,7 @@ pcmm_status ppmv_plan_create(ppmv_plan **out, int64_t M, int64_t K, int32_t grou
         for (int64_t at = 0; at < count; at += most) {
             const int64_t n = count - at < most ? count - at : most;
             hipLaunchKernelGGL(pack_params_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const uint16_t *)scales_dev,
-                               (const uint16_t *)offsets_dev, p->params, M, (K + group - 1) / group, groups_up, at, n);
+                               (const uint16_t *)offsets_dev, p->params, M, (K + group - 1) / group, kblocks, 128 / group, at, n);
         }
         if (hipGetLastError() != hipSuccess || hipStreamSynchronize(st) != hipSuccess) rc = PCMM_EDEVICE;
     }

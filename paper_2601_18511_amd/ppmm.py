@@ -127,37 +127,38 @@ def ppmv_plan_destroy(plan: PpmvPlan) -> None:
     plan.destroy()
 
 
-def _check_product(plan: PpmvPlan, x: torch.Tensor, y: torch.Tensor) -> None:
-    if plan.handle is None:
-        raise ValueError("plan was destroyed")
-    for name, t, width in (("x", x, plan.K), ("the result", y, plan.M)):
-        if not t.is_cuda or t.get_device() != plan.device or t.dtype != plan.dtype:
-            raise ValueError("%s must have the plan's type and device" % name)
-        if t.dim() != 2 or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-            raise ValueError("%s must be [T][%d] with neighbouring elements in a row" % (name, width))
-    if x.shape[0] != y.shape[0]:
-        raise ValueError("x and the result must have the same number of rows")
-
-
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _rows(plan: PpmvPlan, name: str, t: torch.Tensor, width: int):
+    """(rows, address, row stride) of a [T][width] tensor of the plan's type and device with neighbouring elements in a row"""
+    if t.dtype is not plan.dtype or t.get_device() != plan.device:
+        raise ValueError("%s must have the plan's type and device" % name)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != width or (stride[1] != 1 and width > 1):
+        raise ValueError("%s must be [T][%d] with neighbouring elements in a row" % (name, width))
+    return shape[0], t.data_ptr(), stride[0] if shape[0] > 1 else width
 
 
 def ppmv_run(plan: PpmvPlan, x: torch.Tensor, y: torch.Tensor, stream=None) -> None:
     """Enqueue y = x W^T: x is [T][K], y [T][M], both may have longer rows (any row stride). Asynchronous."""
-    _check_product(plan, x, y)
-    rc = load_library().ppmv_run(plan.handle, x.shape[0], x.data_ptr(), _row_stride(x), y.data_ptr(), _row_stride(y), _handle(plan.device, stream))
+    if plan.handle is None:
+        raise ValueError("plan was destroyed")
+    T, px, ldx = _rows(plan, "x", x, plan.K)
+    Ty, py, ldy = _rows(plan, "y", y, plan.M)
+    if T != Ty:
+        raise ValueError("x and y must have the same number of rows")
+    rc = (_lib or load_library()).ppmv_run(plan.handle, T, px, ldx, py, ldy, _handle(plan.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppmv_run")
 
 
 def ppmv_gated_run(gate: PpmvPlan, up: PpmvPlan, x: torch.Tensor, h: torch.Tensor, stream=None) -> None:
     """Enqueue h = silu(x Wg^T) * (x Wu^T): x is [T][K], h [T][M]. Asynchronous."""
-    _check_product(gate, x, h)
-    if up.handle is None:
+    if gate.handle is None or up.handle is None:
         raise ValueError("plan was destroyed")
-    rc = load_library().ppmv_gated_run(gate.handle, up.handle, x.shape[0], x.data_ptr(), _row_stride(x), h.data_ptr(), _row_stride(h),
-                                       _handle(gate.device, stream))
+    T, px, ldx = _rows(gate, "x", x, gate.K)
+    Th, ph, ldh = _rows(gate, "h", h, gate.M)
+    if T != Th:
+        raise ValueError("x and h must have the same number of rows")
+    rc = (_lib or load_library()).ppmv_gated_run(gate.handle, up.handle, T, px, ldx, ph, ldh, _handle(gate.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppmv_gated_run")
 
