@@ -275,6 +275,112 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
     }
 }
 
+// ---- many tokens ---------------------------------------------------------------------------------------------------
+// MFMA-bound.  A work-group of 2 x 2 waves takes 128 rows (64 of either matrix, if gated) and 128 tokens, a wave 64 x 64; x goes
+// through LDS in blocks of 128 k, two of them in turn, and codes go straight from memory to the registers of the wave that
+// unpacks them.  The 16-byte pieces of a token's row lie in LDS at place p ^ (token % 16): the sixteen rows that a read takes
+// them from are on different banks.
+constexpr int kTileRows = 128, kTileTokens = 128;
+
+template <class T, int kGroups, bool kGated, bool kOffsets>
+__global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens, uint32_t row_tiles,
+                                                             uint32_t token_tiles, const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+{
+    using Par = Params<kGroups, kOffsets>;
+    constexpr int kSteps = 4 / kGroups, kMats = kGated ? 2 : 1, kRows = 4 / kMats;
+    __shared__ u32x4 tile[2][kTileTokens * 16];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
+    // An XCD gets neighbouring tiles: eight tiles of tokens and all rows, then the next eight.
+    const uint32_t all = row_tiles * token_tiles, share = (all + 7) / 8;
+    const uint32_t id = blockIdx.x % 8 * share + blockIdx.x / 8;
+    if (id >= all) return;                          // the whole work-group
+    const uint32_t strip = id / (8 * row_tiles), width = token_tiles - 8 * strip < 8 ? token_tiles - 8 * strip : 8, in = id - strip * 8 * row_tiles;
+    const int64_t t0 = (int64_t)(8 * strip + in % width) * kTileTokens, first = (int64_t)(in / width) * (kTileRows / 16 / kMats) + wave / 2 * kRows;
+    const int64_t tiles = (M + 15) / 16;
+    const u32x4 *codes_of[4];
+    const uint16_t *params_of[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                   // a tile behind the last one is the last one once more
+        const Weights &w = i / kRows ? b : a;
+        const int64_t at = first + i % kRows < tiles ? first + i % kRows : tiles - 1;
+        codes_of[i] = w.codes + at * kblocks * 64 + lane;
+        params_of[i] = w.params + at * kblocks * Par::kStride;
+    }
+    // x: a thread brings the piece threadIdx % 16 of every sixteenth token; tokens behind the last one are the last one
+    const int piece = threadIdx.x % 16, token = threadIdx.x / 16;
+    u32x4 next[8], codes[4];
+    Par params[4];
+    const auto fetch = [&](int kb) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const int64_t t = t0 + token + 16 * n < tokens ? t0 + token + 16 * n : tokens - 1;
+            next[n] = load_x(x + t * ldx, (int64_t)kb * 128 + 8 * piece, K, aligned);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            codes[i] = codes_of[i][(int64_t)kb * 64];
+            params[i].load(params_of[i] + (int64_t)kb * Par::kStride, h);
+        }
+    };
+    f32x4 sum[4][4] = {};
+    fetch(0);
+    for (int kb = 0; kb < kblocks; ++kb) {
+        u32x4 *buf = tile[kb % 2];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) buf[(token + 16 * n) * 16 + (piece ^ token)] = next[n];
+        u32x4 v[4][4];
+        f32x4 s[4][kGroups], o[4][kGroups];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = ppmm::unpack<T>(codes[i][j]);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                s[i][g] = four<T>(params[i].v[g * Par::kKinds]);
+                if constexpr (kOffsets) o[i][g] = four<T>(params[i].v[g * 2 + 1]) * (-1.0f / 24.0f);
+            }
+        }
+        __syncthreads();
+        if (kb + 1 < kblocks) fetch(kb + 1);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            u32x4 xs[4];
+            const u32x4 *from = buf + (wave % 2 * 64 + 16 * t + col) * 16;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xs[j] = from[(4 * j + h) ^ col];
+            f32x4 base[kGroups];
+            group_sums<T, kGroups>(base, xs);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                f32x4 acc[4];
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i] = T::mma(v[i][g * kSteps + j], xs[g * kSteps + j], j ? acc[i] : base[g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sum[i][t][e] = fmaf(s[i][g][e], acc[i][e], sum[i][t][e]);
+                        if constexpr (kOffsets) sum[i][t][e] = fmaf(o[i][g][e], base[g][e], sum[i][t][e]);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int64_t n = t0 + wave % 2 * 64 + 16 * t + col;
+        if (n >= tokens) continue;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t m = (first + i) * 16 + 4 * h + e;
+                if (m < M) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(sum[i][t][e], sum[i + kRows * (kMats - 1)][t][e]) : sum[i][t][e]);
+            }
+    }
+}
+
 struct Call {
     const ppmv_plan *p, *u;
     int64_t T;
@@ -307,8 +413,21 @@ template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(cons
                        kblocks, (int)c.T, c.x, c.ldx, aligned16(c), c.y, c.ldy);
 }
 
+template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
+{
+    const ppmv_plan *p = c.p, *u = c.u;
+    const int64_t rows = kGated ? kTileRows / 2 : kTileRows;
+    const uint32_t row_tiles = (uint32_t)((p->M + rows - 1) / rows), token_tiles = (uint32_t)((c.T + kTileTokens - 1) / kTileTokens);
+    const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
+    auto kernel = p->has_offsets ? many_tokens_kernel<T, kGroups, kGated, true> : many_tokens_kernel<T, kGroups, kGated, false>;
+    // check_product: fewer than 2^24 tiles of 16 x 64, so these count in 32 bits and launch fewer than 2^32 threads
+    hipLaunchKernelGGL(kernel, dim3((row_tiles * token_tiles + 7) / 8 * 8), dim3(256), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, row_tiles,
+                       token_tiles, c.x, c.ldx, aligned16(c), c.y, c.ldy);
+}
+
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
 {
+    if (c.T > 64) return launch_many<T, kGroups, kGated>(c);
     if (c.T <= 4 && c.T * c.p->K <= 16384) {
         // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
         // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.  (Two matrices in groups of 32 do not fit the registers then.)
