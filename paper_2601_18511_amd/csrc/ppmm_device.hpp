@@ -40,16 +40,20 @@ struct FP16 {
 __device__ inline uint32_t rotate_right(uint32_t v, int by) { return __builtin_amdgcn_alignbit(v, v, by); }
 
 // Eight codes -> eight values 16 + code.  Of the word's nibbles, counted from bit kCodeBit on and around the end, number i and
-// number 4 + i become the pair i: a rotation and a mask-and-or each.
-template <class T> __device__ inline u32x4 unpack(uint32_t w)
-{
-    constexpr uint32_t mask = 0x000F000Fu << T::kCodeBit;
-    u32x4 v;
-    v[0] = (w & mask) | T::kSixteen;
+// number 4 + i become the pair i: a rotation and a mask-and-or each.  The instruction takes one constant from a scalar register, so
+// the other one is kept in a vector register (as literals the compiler splits it in two, 11 instructions for 7).
+template <class T> struct Unpacker {
+    uint32_t mask, sixteen;
+    __device__ inline Unpacker() : mask(0x000F000Fu << T::kCodeBit), sixteen(T::kSixteen) { asm("" : "+s"(mask), "+v"(sixteen)); }
+    __device__ inline u32x4 operator()(uint32_t w) const
+    {
+        u32x4 v;
+        v[0] = (w & mask) | sixteen;
 #pragma unroll
-    for (int i = 1; i < 4; ++i) v[i] = (rotate_right(w, 4 * i) & mask) | T::kSixteen;
-    return v;
-}
+        for (int i = 1; i < 4; ++i) v[i] = (rotate_right(w, 4 * i) & mask) | sixteen;
+        return v;
+    }
+};
 
 template <class T> __device__ inline float to_f32(uint16_t bits) { return (float)__builtin_bit_cast(typename T::type, bits); }
 template <class T> __device__ inline uint16_t from_f32(float v) { return __builtin_bit_cast(uint16_t, (typename T::type)v); }   // to nearest even

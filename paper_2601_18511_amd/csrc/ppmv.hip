@@ -76,14 +76,15 @@ __global__ __launch_bounds__(256) void pack_params_kernel(const uint16_t *scales
 // HBM-bound: the weights stream through once and every token rides along.  A work-group of kWaves waves takes kRows tiles of 16
 // rows (of both matrices, if gated) and kTok tiles of 16 tokens; its waves share out the blocks of K and add up through LDS.
 
-// eight values of one token from k on, zero behind K
-__device__ inline u32x4 load_x(const uint16_t *row, int64_t k, int64_t K, bool aligned)
+// Eight values of one token from k on, zero behind K.  Elements are aligned to two bytes; the loads take any such address.
+__device__ inline u32x4 load_x(const uint16_t *row, int64_t k, int64_t K)
 {
     u32x4 v = {0, 0, 0, 0};
-    if (aligned && k + 8 <= K) return *(const u32x4 *)(row + k);
+    if (k + 8 <= K) __builtin_memcpy(&v, row + k, 16);
+    else
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (k + i < K) v[i / 2] |= (uint32_t)row[k + i] << (16 * (i % 2));
+        for (int i = 0; i < 8; ++i)
+            if (k + i < K) v[i / 2] |= (uint32_t)row[k + i] << (16 * (i % 2));
     return v;
 }
 
@@ -126,7 +127,7 @@ template <class T, int kGroups> __device__ inline void group_sums(f32x4 (&base)[
 
 // sum += block times the kTok tiles of x
 template <class T, int kTok, int kGroups, bool kOffsets>
-__device__ inline void add_block(f32x4 (&sum)[kTok], u32x4 codes, const Params<kGroups, kOffsets> &p, const u32x4 (&x)[kTok][4],
+__device__ inline void add_block(const ppmm::Unpacker<T> &unpack, f32x4 (&sum)[kTok], u32x4 codes, const Params<kGroups, kOffsets> &p, const u32x4 (&x)[kTok][4],
                                  const f32x4 (&base)[kTok][kGroups])
 {
     constexpr int kSteps = 4 / kGroups, kKinds = kOffsets ? 2 : 1;
@@ -135,7 +136,7 @@ __device__ inline void add_block(f32x4 (&sum)[kTok], u32x4 codes, const Params<k
         f32x4 acc[kTok];
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            const u32x4 v = ppmm::unpack<T>(codes[g * kSteps + j]);
+            const u32x4 v = unpack(codes[g * kSteps + j]);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) acc[t] = T::mma(v, x[t][g * kSteps + j], j ? acc[t] : base[t][g]);
         }
@@ -180,7 +181,7 @@ __device__ inline void finish(const f32x4 (&part)[kWaves][kRows * (kGated ? 2 : 
 // more blocks ahead (2 or 4) took registers and with them waves: 14336 x 4096 gated, group 64, 14.6 and 15.5 us for 14.0.
 template <class T, int kWaves, int kGroups, bool kGated, bool kOffsets>
 __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights b, int64_t M, int K, int kblocks, int tokens, const uint16_t *x,
-                                                             int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+                                                             int64_t ldx, uint16_t *y, int64_t ldy)
 {
     constexpr int kMats = kGated ? 2 : 1;
     using Par = Params<kGroups, kOffsets>;
@@ -201,9 +202,10 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
     if (wave < kblocks) fetch(wave);
     const int pitch = kblocks * 16 + 1;             // the odd one keeps the rows on different banks
     for (int t = 0; t < tokens; ++t)
-        for (int i = threadIdx.x; i < kblocks * 16; i += 64 * kWaves) rows[t * pitch + i] = load_x(x + t * ldx, 8 * i, K, aligned);
+        for (int i = threadIdx.x; i < kblocks * 16; i += 64 * kWaves) rows[t * pitch + i] = load_x(x + t * ldx, 8 * i, K);
     __syncthreads();
     const u32x4 *mine = rows + (col < tokens ? col : tokens - 1) * pitch + h;
+    const ppmm::Unpacker<T> unpack;
     f32x4 sum[kMats][1] = {};
     for (int kb = wave; kb < kblocks; kb += kWaves) {
         u32x4 xs[1][4];
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
         f32x4 base[1][kGroups];
         group_sums<T, kGroups>(base[0], xs[0]);
 #pragma unroll
-        for (int w = 0; w < kMats; ++w) add_block<T, 1, kGroups, kOffsets>(sum[w], codes[w], params[w], xs, base);
+        for (int w = 0; w < kMats; ++w) add_block<T, 1, kGroups, kOffsets>(unpack, sum[w], codes[w], params[w], xs, base);
         if (kb + kWaves < kblocks) fetch(kb + kWaves);
     }
 #pragma unroll
@@ -224,13 +226,14 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
 // Any number of tokens; x comes from the caches as the matrix instruction wants it.
 template <class T, int kTok, int kRows, int kWaves, int kGroups, bool kGated, bool kOffsets>
 __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens,
-                                                                 const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+                                                                 const uint16_t *x, int64_t ldx, uint16_t *y, int64_t ldy)
 {
     constexpr int kTiles = kRows * (kGated ? 2 : 1);
     using Par = Params<kGroups, kOffsets>;
     __shared__ f32x4 part[kWaves][kTiles][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
     const int64_t tiles = (M + 15) / 16, tile0 = (int64_t)blockIdx.x * kRows, t0 = (int64_t)blockIdx.y * 16 * kTok;
+    const ppmm::Unpacker<T> unpack;
     f32x4 sum[kTiles][kTok] = {};
     const u32x4 *codes_of[kTiles];
     const uint16_t *params_of[kTiles];
@@ -257,13 +260,13 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 xs[t][j] = u32x4{0, 0, 0, 0};
-                if (t0 + 16 * t + col < tokens) xs[t][j] = load_x(row[t], (int64_t)kb * 128 + 32 * j + 8 * h, K, aligned);
+                if (t0 + 16 * t + col < tokens) xs[t][j] = load_x(row[t], (int64_t)kb * 128 + 32 * j + 8 * h, K);
             }
         f32x4 base[kTok][kGroups];
 #pragma unroll
         for (int t = 0; t < kTok; ++t) group_sums<T, kGroups>(base[t], xs[t]);
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) add_block<T, kTok, kGroups, kOffsets>(sum[i], codes[i], params[i], xs, base);
+        for (int i = 0; i < kTiles; ++i) add_block<T, kTok, kGroups, kOffsets>(unpack, sum[i], codes[i], params[i], xs, base);
     }
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
@@ -281,6 +284,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
 // unpacks them.  The 16-byte pieces of a token's row lie in LDS at place p ^ (token % 16): the sixteen rows that a read takes
 // them from are on different banks.
 constexpr int kTileRows = 128, kTileTokens = 128;
+
+// 64 lanes' 16 bytes from memory to 1 KiB of LDS, without a register in between
+__device__ inline void load_to_lds(const void *from, u32x4 *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from, (__attribute__((address_space(3))) uint32_t *)to, 16, 0, 0);
+}
 
 template <class T, int kGroups, bool kGated, bool kOffsets>
 __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens, uint32_t row_tiles,
@@ -303,66 +312,70 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
     for (int i = 0; i < 4; ++i) {                   // a tile behind the last one is the last one once more
         const Weights &w = i / kRows ? b : a;
         const int64_t at = first + i % kRows < tiles ? first + i % kRows : tiles - 1;
-        codes_of[i] = w.codes + at * kblocks * 64 + lane;
+        codes_of[i] = w.codes + at * kblocks * 64;
         params_of[i] = w.params + at * kblocks * Par::kStride;
     }
-    // x: a thread brings the piece threadIdx % 16 of every sixteenth token; tokens behind the last one are the last one
-    const int piece = threadIdx.x % 16, token = threadIdx.x / 16;
-    u32x4 next[8], codes[4];
+    // x: a wave brings 32 tokens, four at a time, a lane the piece that belongs at its own place; tokens behind the last one are the last one
+    const auto stage = [&](int kb) {
+        u32x4 *to = tile[kb % 2] + wave * 32 * 16;
+        const bool whole = aligned && (int64_t)(kb + 1) * 128 <= K;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const int token = wave * 32 + 4 * n + lane / 16, piece = lane % 16 ^ token % 16;
+            const int64_t t = t0 + token < tokens ? t0 + token : tokens - 1, k = (int64_t)kb * 128 + 8 * piece;
+            if (whole) load_to_lds(x + t * ldx + k, to + 64 * n);
+            else to[64 * n + lane] = load_x(x + t * ldx, k, K);
+        }
+    };
+    u32x4 codes[4];
     Par params[4];
     const auto fetch = [&](int kb) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const int64_t t = t0 + token + 16 * n < tokens ? t0 + token + 16 * n : tokens - 1;
-            next[n] = load_x(x + t * ldx, (int64_t)kb * 128 + 8 * piece, K, aligned);
-        }
-#pragma unroll
         for (int i = 0; i < 4; ++i) {
-            codes[i] = codes_of[i][(int64_t)kb * 64];
+            codes[i] = (codes_of[i] + (int64_t)kb * 64)[lane];
             params[i].load(params_of[i] + (int64_t)kb * Par::kStride, h);
         }
     };
+    const ppmm::Unpacker<T> unpack;
     f32x4 sum[4][4] = {};
+    stage(0);
     fetch(0);
     for (int kb = 0; kb < kblocks; ++kb) {
-        u32x4 *buf = tile[kb % 2];
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wave's part of the block is in LDS
+        __syncthreads();                                        // everyone's is, and nobody reads the other block any more
+        if (kb + 1 < kblocks) stage(kb + 1);
+        const u32x4 *from = tile[kb % 2] + (wave % 2 * 64 + col) * 16;
 #pragma unroll
-        for (int n = 0; n < 8; ++n) buf[(token + 16 * n) * 16 + (piece ^ token)] = next[n];
-        u32x4 v[4][4];
-        f32x4 s[4][kGroups], o[4][kGroups];
+        for (int g = 0; g < kGroups; ++g) {
+            u32x4 v[4][kSteps];
+            f32x4 s[4], o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] = ppmm::unpack<T>(codes[i][j]);
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                s[i][g] = four<T>(params[i].v[g * Par::kKinds]);
-                if constexpr (kOffsets) o[i][g] = four<T>(params[i].v[g * 2 + 1]) * (-1.0f / 24.0f);
+                for (int j = 0; j < kSteps; ++j) v[i][j] = unpack(codes[i][g * kSteps + j]);
+                s[i] = four<T>(params[i].v[g * Par::kKinds]);
+                if constexpr (kOffsets) o[i] = four<T>(params[i].v[g * 2 + 1]) * (-1.0f / 24.0f);
             }
-        }
-        __syncthreads();
-        if (kb + 1 < kblocks) fetch(kb + 1);
+            if (g == kGroups - 1 && kb + 1 < kblocks) fetch(kb + 1);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            u32x4 xs[4];
-            const u32x4 *from = buf + (wave % 2 * 64 + 16 * t + col) * 16;
+            for (int t = 0; t < 4; ++t) {
+                u32x4 xs[kSteps];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xs[j] = from[(4 * j + h) ^ col];
-            f32x4 base[kGroups];
-            group_sums<T, kGroups>(base, xs);
+                for (int j = 0; j < kSteps; ++j) xs[j] = from[16 * t * 16 + ((4 * (g * kSteps + j) + h) ^ col)];
+                const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
+                f32x4 base = {0, 0, 0, 0}, acc[4];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                f32x4 acc[4];
+                for (int j = 0; j < kSteps; ++j) base = T::mma(minus24, xs[j], base);
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] = T::mma(v[i][g * kSteps + j], xs[g * kSteps + j], j ? acc[i] : base[g]);
+                    for (int i = 0; i < 4; ++i) acc[i] = T::mma(v[i][j], xs[j], j ? acc[i] : base);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        sum[i][t][e] = fmaf(s[i][g][e], acc[i][e], sum[i][t][e]);
-                        if constexpr (kOffsets) sum[i][t][e] = fmaf(o[i][g][e], base[g][e], sum[i][t][e]);
+                        sum[i][t][e] = fmaf(s[i][e], acc[i][e], sum[i][t][e]);
+                        if constexpr (kOffsets) sum[i][t][e] = fmaf(o[i][e], base[e], sum[i][t][e]);
                     }
             }
         }
@@ -400,7 +413,7 @@ template <class T, int kTok, int kRows, int kGroups, bool kGated> void launch_fe
     const dim3 grid((unsigned)((tiles + kRows - 1) / kRows), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, true> : few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, aligned16(c), c.y, c.ldy);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, c.y, c.ldy);
 }
 
 template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(const Call &c)
@@ -410,7 +423,7 @@ template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(cons
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? stream_kernel<T, kWaves, kGroups, kGated, true> : stream_kernel<T, kWaves, kGroups, kGated, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((p->M + 15) / 16)), dim3(64 * kWaves), (size_t)c.T * (kblocks * 16 + 1) * 16, c.stream, a, b, p->M, (int)p->K,
-                       kblocks, (int)c.T, c.x, c.ldx, aligned16(c), c.y, c.ldy);
+                       kblocks, (int)c.T, c.x, c.ldx, c.y, c.ldy);
 }
 
 template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
