@@ -101,6 +101,7 @@ __device__ inline float silu_times(float g, float u)
 // Scales and offsets of one block: kGroups groups of the lane's four rows.
 template <int kGroups, bool kOffsets> struct Params {
     static constexpr int kKinds = kOffsets ? 2 : 1, kStride = kGroups * kKinds * 16;      // 16-bit words of a block
+    static constexpr int kLoads = kGroups * kKinds > 1 ? kGroups * kKinds / 2 : 1;
     u32x2 v[kGroups * kKinds];
     __device__ inline void load(const uint16_t *block, int h)
     {
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
     const int64_t tile = blockIdx.x;
     u32x4 codes[kMats];
     Par params[kMats];
-    const auto fetch = [&](int kb) {
+    const auto fetch = [&](int kb) __attribute__((always_inline)) {
 #pragma unroll
         for (int w = 0; w < kMats; ++w) {
             const Weights &m = w ? b : a;
@@ -285,15 +286,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
 // them from are on different banks.
 constexpr int kTileRows = 128, kTileTokens = 128;
 
-// 64 lanes' 16 bytes from memory to 1 KiB of LDS, without a register in between
-__device__ inline void load_to_lds(const void *from, u32x4 *to)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from, (__attribute__((address_space(3))) uint32_t *)to, 16, 0, 0);
-}
-
 template <class T, int kGroups, bool kGated, bool kOffsets>
 __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens, uint32_t row_tiles,
-                                                             uint32_t token_tiles, const uint16_t *x, int64_t ldx, bool aligned, uint16_t *y, int64_t ldy)
+                                                             uint32_t token_tiles, const uint16_t *x, int64_t ldx, bool buffered, uint16_t *y, int64_t ldy)
 {
     using Par = Params<kGroups, kOffsets>;
     constexpr int kSteps = 4 / kGroups, kMats = kGated ? 2 : 1, kRows = 4 / kMats;
@@ -315,35 +310,53 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
         codes_of[i] = w.codes + at * kblocks * 64;
         params_of[i] = w.params + at * kblocks * Par::kStride;
     }
-    // x: a wave brings 32 tokens, four at a time, a lane the piece that belongs at its own place; tokens behind the last one are the last one
-    const auto stage = [&](int kb) {
+    // x: a wave brings 32 tokens, four at a time, a lane the piece that belongs at its own place.  Whole blocks go to LDS without a
+    // register in between; the buffer ends with the tile's last token, and what lies behind reads as zero.
+    const int64_t held = tokens - t0 < kTileTokens ? tokens - t0 : kTileTokens;
+    const auto rows = __builtin_amdgcn_make_buffer_rsrc((void *)(x + t0 * ldx), 0, buffered ? (int)(((held - 1) * ldx + K) * 2) : 0, 0x00027000);
+    const auto stage = [&](int kb) __attribute__((always_inline)) {
         u32x4 *to = tile[kb % 2] + wave * 32 * 16;
-        const bool whole = aligned && (int64_t)(kb + 1) * 128 <= K;
+        // opaque, so that nothing of the addresses is kept in registers from one block to the next
+        int l = lane;
+        const uint16_t *from = x;
+        asm volatile("" : "+v"(l), "+s"(from));
+        if (buffered && (kb + 1) * 128 <= K) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const int token = wave * 32 + 4 * n + lane / 16, piece = lane % 16 ^ token % 16;
-            const int64_t t = t0 + token < tokens ? t0 + token : tokens - 1, k = (int64_t)kb * 128 + 8 * piece;
-            if (whole) load_to_lds(x + t * ldx + k, to + 64 * n);
-            else to[64 * n + lane] = load_x(x + t * ldx, k, K);
+            for (int n = 0; n < 8; ++n)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)(to + 64 * n), 16,
+                                                         (wave * 32 + 4 * n + l / 16) * (int)ldx * 2 + ((l % 16 ^ (4 * n + l / 16) % 16) * 8 + kb * 128) * 2, 0, 0, 0);
+        } else {
+#pragma unroll 1
+            for (int n = 0; n < 8; ++n) {
+                const int token = wave * 32 + 4 * n + l / 16;
+                to[64 * n + l] = token < held ? load_x(from + (t0 + token) * ldx, (int64_t)kb * 128 + 8 * (l % 16 ^ token % 16), K) : u32x4{0, 0, 0, 0};
+            }
         }
     };
     u32x4 codes[4];
     Par params[4];
-    const auto fetch = [&](int kb) {
+    const auto fetch = [&](int kb) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             codes[i] = (codes_of[i] + (int64_t)kb * 64)[lane];
             params[i].load(params_of[i] + (int64_t)kb * Par::kStride, h);
         }
     };
+    const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
     const ppmm::Unpacker<T> unpack;
     f32x4 sum[4][4] = {};
     stage(0);
+    asm volatile("" ::: "memory");
     fetch(0);
     for (int kb = 0; kb < kblocks; ++kb) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wave's part of the block is in LDS
+        // this wave's part of the block is in LDS; the loads of weights behind it may be under way
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 + 4 * Par::kLoads) : "memory");
         __syncthreads();                                        // everyone's is, and nobody reads the other block any more
+        // Loads are counted in their order: the wait for this block's codes stands here, in front of the next loads of x, or it would
+        // be a wait for those too; and the next codes come behind them.
+        asm volatile("" : "+v"(codes[0]), "+v"(codes[1]), "+v"(codes[2]), "+v"(codes[3]));
         if (kb + 1 < kblocks) stage(kb + 1);
+        asm volatile("" ::: "memory");
         const u32x4 *from = tile[kb % 2] + (wave % 2 * 64 + col) * 16;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
@@ -356,13 +369,12 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
                 s[i] = four<T>(params[i].v[g * Par::kKinds]);
                 if constexpr (kOffsets) o[i] = four<T>(params[i].v[g * 2 + 1]) * (-1.0f / 24.0f);
             }
-            if (g == kGroups - 1 && kb + 1 < kblocks) fetch(kb + 1);
+            if (g == kGroups - 1) fetch(kb + 1 < kblocks ? kb + 1 : kb);      // without a branch: sums would sink below it
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 u32x4 xs[kSteps];
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j) xs[j] = from[16 * t * 16 + ((4 * (g * kSteps + j) + h) ^ col)];
-                const u32x4 minus24 = {T::kMinus24, T::kMinus24, T::kMinus24, T::kMinus24};
                 f32x4 base = {0, 0, 0, 0}, acc[4];
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j) base = T::mma(minus24, xs[j], base);
@@ -377,7 +389,10 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
                         sum[i][t][e] = fmaf(s[i][e], acc[i][e], sum[i][t][e]);
                         if constexpr (kOffsets) sum[i][t][e] = fmaf(o[i][e], base[e], sum[i][t][e]);
                     }
+                if constexpr (kGroups == 4) if (t == 1) __builtin_amdgcn_sched_barrier(0);
             }
+            // the compiler otherwise starts on the other groups at once and runs out of registers
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 #pragma unroll
@@ -403,8 +418,6 @@ struct Call {
     int64_t ldy;
     hipStream_t stream;
 };
-
-bool aligned16(const Call &c) { return ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0; }
 
 template <class T, int kTok, int kRows, int kGroups, bool kGated> void launch_few(const Call &c)
 {
@@ -433,9 +446,10 @@ template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
     const uint32_t row_tiles = (uint32_t)((p->M + rows - 1) / rows), token_tiles = (uint32_t)((c.T + kTileTokens - 1) / kTileTokens);
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? many_tokens_kernel<T, kGroups, kGated, true> : many_tokens_kernel<T, kGroups, kGated, false>;
+    const bool buffered = ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0 && c.ldx < (1 << 22);      // aligned pieces, 32-bit offsets in a tile
     // check_product: fewer than 2^24 tiles of 16 x 64, so these count in 32 bits and launch fewer than 2^32 threads
     hipLaunchKernelGGL(kernel, dim3((row_tiles * token_tiles + 7) / 8 * 8), dim3(256), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, row_tiles,
-                       token_tiles, c.x, c.ldx, aligned16(c), c.y, c.ldy);
+                       token_tiles, c.x, c.ldx, buffered, c.y, c.ldy);
 }
 
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
