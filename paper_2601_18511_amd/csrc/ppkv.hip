@@ -6,6 +6,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ppmm_device.hpp"
 #include "ppmm_host.hpp"
 #include "pcmm_hip_util.hpp"
@@ -14,16 +16,37 @@ namespace {
 
 using ppmm::BF16;
 using ppmm::Cache;
+using ppmm::f32x4;
 using ppmm::FP16;
+using ppmm::u32x4;
 
 constexpr int kThreads = 256;
 
-// Places inside a page of one head.  A token's D/2 bytes of codes are words of eight codes, ascending channels from the lowest
-// four bits.  Values lie in order.  The words of a key are transposed: word (D/32) h + j holds channels 32 j + 8 h ... + 7.
+// Places inside a page of one head.  A token's D/2 bytes of codes are words of eight codes; the words of a value lie in order, its
+// channels from the lowest four bits up.  The words of a key are transposed: word (D/32) h + j holds channels 32 j + 8 h ... + 7, so
+// that a lane of the matrix instruction (quarter h) reads its words of all groups at once; of the eight channels the even ones are
+// nibbles 0..3 and the odd ones 4..7, and the word is rotated by three bits, as Unpacker wants them.  A token's scales (one for
+// each group) lie in front of its offsets.
+constexpr int kKeyBit = BF16::kCodeBit;
+
 template <int D> __device__ inline int64_t codes_at(const Cache &c, int which, int slot) { return (int64_t)(which * c.page_size + slot) * (D / 2); }
 template <int D> __device__ inline int64_t params_at(const Cache &c, int which, int slot)
 {
     return (int64_t)c.page_size * D + (int64_t)(which * c.page_size + slot) * (D / 8);
+}
+
+// word of eight codes, in the order of the channels, as a key's word, and back
+__device__ inline uint32_t key_word(uint32_t w)
+{
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v |= (w >> (8 * i) & 15) << (4 * i) | (w >> (8 * i + 4) & 15) << (4 * i + 16);
+    return v << kKeyBit | v >> (32 - kKeyBit);
+}
+__device__ inline uint32_t code_of(uint32_t word, int which, int i)       // channel i of the word
+{
+    if (which) return word >> (4 * i) & 15;
+    return ppmm::rotate_right(word, (4 * (i / 2) + 16 * (i % 2) + kKeyBit) % 32) & 15;
 }
 
 // ---- writing -------------------------------------------------------------------------------------------------------
@@ -76,8 +99,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Cache c, int64_t token
     const int slot = (int)(position % c.page_size);
     const int j = part / 4, h = part % 4;
     const int place = which ? part : (D / 32) * h + j;
-    *(uint32_t *)(page + codes_at<D>(c, which, slot) + 4 * place) = word;
-    if (h == 0) *(uint32_t *)(page + params_at<D>(c, which, slot) + 4 * j) = s_bits | (uint32_t)b_bits << 16;
+    *(uint32_t *)(page + codes_at<D>(c, which, slot) + 4 * place) = which ? word : key_word(word);
+    uint16_t *params = (uint16_t *)(page + params_at<D>(c, which, slot));
+    if (h == 0) params[j] = s_bits;
+    if (h == 1) params[D / 32 + j] = b_bits;
 }
 
 // ---- reading -------------------------------------------------------------------------------------------------------
@@ -107,66 +132,430 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
     const uint8_t *page = c.page_of(b, position, head);
     uint16_t *dst = (which ? v + n * vts + head * vhs : k + n * kts + head * khs) + part * 8;
     const int j = part / 4, h = part % 4;
-    uint32_t word = 0, sb = 0;
+    uint32_t word = 0;
+    float s = 0.0f, off = 0.0f;
     if (page) {
         const int slot = (int)(position % c.page_size);
         word = *(const uint32_t *)(page + codes_at<D>(c, which, slot) + 4 * (which ? part : (D / 32) * h + j));
-        sb = *(const uint32_t *)(page + params_at<D>(c, which, slot) + 4 * j);
+        const uint16_t *params = (const uint16_t *)(page + params_at<D>(c, which, slot));
+        s = ppmm::to_f32<BF16>(params[j]);
+        off = ppmm::to_f32<BF16>(params[D / 32 + j]);
     }
-    const float s = ppmm::to_f32<BF16>((uint16_t)sb), off = ppmm::to_f32<BF16>((uint16_t)(sb >> 16));
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        dst[i] = as_result<T>(fmaf(s, 16.0f + (float)(word >> (4 * i) & 15), off), fixed);
+        dst[i] = as_result<T>(fmaf(s, 16.0f + (float)code_of(word, which, i), off), fixed);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------
-// One wave a row and head, one key after the other.
-template <class T, int D>
-__global__ __launch_bounds__(64) void attention_kernel(Cache c, int64_t tokens, int32_t heads, const uint16_t *q, int64_t qts, int64_t qhs,
-                                                       uint16_t *out, int64_t ots, int64_t ohs, float scale, int32_t causal, int32_t max_q)
+// Tiles of 64 keys, 16 at a time as the rows of a matrix product with queries as its columns.  Nothing is dequantised:
+//
+//   score     sum_j s_j (sum_{c in j} q_c (16 + code_c))  +  sum_j b_j sum_{c in j} q_c
+//   output    sum_i (p_i s_ij) (16 + code_ic)             +  sum_i p_i b_ij              for a channel c of group j
+//
+// q (16 + code) is exact; p s enters in two bf16 halves of 8 bits each.  A key's scales and offsets are 16 bytes, which are an
+// operand of the matrix instruction as they are: times a one they come out in the layout of the scores, times the groups' sums of q (in
+// three bf16 parts) they are the score's second sum.  The values' codes go through LDS, whose transposing read hands a lane
+// sixteen keys of one channel.  The sixteen keys are those whose scores the lane holds, so probabilities stay where they are.
+//
+// Few queries (kFew): a column is a pair of group and query, 16 / (D/32) queries a tile: the products of all groups with their
+// scales are one instruction each, and lanes do not work on empty columns.  Otherwise a column is a query, and the groups follow one
+// another; the scale of group j then comes out in every (D/32)th column and is taken from there.
+//
+// The four waves of a work-group share out the tiles of its keys and join at the end; where there are few rows, several
+// work-groups share out the keys of a row and a second kernel joins them.
+
+__device__ inline float across_quarters(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+__device__ inline float most_of_quarters(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+template <int kCtrl> __device__ inline float dpp(float v)
 {
-    constexpr int E = D / 64;                       // channels of a lane
-    const int64_t n = blockIdx.x / heads;
-    const int qh = (int)(blockIdx.x % heads), head = qh / (heads / c.kv_heads);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+}
+constexpr int kRor4 = 0x124, kRor8 = 0x128;         // rotations of 16 lanes
+__host__ __device__ constexpr int quad_of(int lane, int period) { return period == 4 ? lane * 0x55 : lane ? 0xDD : 0x88; }   // every lane of a quad takes this one; period 2: of its own pair
+
+__device__ inline uint32_t high_part(float v) { return __builtin_bit_cast(uint32_t, v) & 0xffff0000u; }
+__device__ inline float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ inline uint32_t pack_high(float lo, float hi) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u); }
+__device__ inline uint32_t pack_bf16(float lo, float hi) { return ppmm::from_f32<BF16>(lo) | (uint32_t)ppmm::from_f32<BF16>(hi) << 16; }
+
+// Rows of one sequence and K/V head: row r is new token r / G, head G * kv_head + r % G.
+struct Rows {
+    int64_t first, next, tokens, length, capacity;
+    int32_t G, kv_head;
+    bool causal;
+    __device__ inline int64_t token(int64_t r) const { return first + r / G; }
+    __device__ inline int64_t limit(int64_t r) const        // keys that row r attends to
+    {
+        const int64_t held = length < capacity ? length : capacity, own = length - (next - token(r)) + 1;
+        const int64_t n = causal && own < held ? own : held;
+        return n > 0 ? n : 0;
+    }
+};
+
+// The keys of one split: `of` of them, whole rounds of the four waves.
+__device__ inline int64_t split_size(int64_t length, int splits) { return (((length > 0 ? length : 0) + splits - 1) / splits + 255) / 256 * 256; }
+
+template <class T, int D, int kTiles, bool kFew>
+__global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t tokens, int32_t heads, const uint16_t *q, int64_t qts, int64_t qhs, uint16_t *out,
+                                                           int64_t ots, int64_t ohs, float scale, int32_t causal, int32_t max_q, int32_t splits, float *scratch)
+{
+    constexpr int kGroups = D / 32, kChannelTiles = D / 16, kQueries = kFew ? 16 / kGroups : 16, kRows = kQueries * kTiles;
+    constexpr int kPitch = D / 2 + 16;              // bytes of a token's values in LDS
+    constexpr int kParamWords = D / 32;             // 32-bit words of a token's scales and offsets
+    __shared__ union {                              // the waves' values, and after the last key their results
+        __attribute__((aligned(16))) uint8_t values[4][64 * kPitch];
+        float joined[4][kQueries][D + 4];
+    } lds;
+    __shared__ float stats[2][4][kTiles][16];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
+    const int32_t b = blockIdx.z, split = blockIdx.x % splits;
+    Rows rows{c.starts[b], c.starts[b + 1], tokens, c.lens[b], c.capacity(), heads / c.kv_heads, (int32_t)blockIdx.y, causal != 0};
+    const int64_t news = rows.next - rows.first < max_q ? rows.next - rows.first : max_q, count = news * rows.G;
+    const int64_t row0 = (int64_t)(blockIdx.x / splits) * kRows;
+    if (row0 >= count) return;
+    const int64_t held = rows.length < rows.capacity ? rows.length : rows.capacity, part = split_size(held, splits);
+    const int64_t begin = split * part;
+    if (split > 0 && begin >= held) return;
+    const int64_t last = row0 + kRows < count ? row0 + kRows - 1 : count - 1;
+    int64_t end = rows.limit(last) < begin + part ? rows.limit(last) : begin + part;      // behind the keys of any row
+    const int64_t clear = rows.limit(row0);         // keys in front of this belong to every row
+
+    const int mine = kFew ? col / kQueries : col % kGroups;                  // the group whose scale this column brings out
+    const int query = kFew ? col % kQueries : col;
+    // the column's queries as the second operand, and its sums in three parts, one a quarter of the lanes
+    u32x4 qs[kTiles][kGroups], qsum[kTiles];
+    int64_t limit[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const int64_t r = row0 + t * kQueries + query, n = rows.token(r);
+        const bool live = r < count && n >= 0 && n < tokens;
+        limit[t] = live ? rows.limit(r) : 0;
+        qsum[t] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            u32x4 v = {0, 0, 0, 0};
+            if (live && (!kFew || mine == j)) __builtin_memcpy(&v, q + n * qts + (rows.kv_head * rows.G + r % rows.G) * qhs + 32 * j + 8 * h, 16);
+            qs[t][j] = v;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += ppmm::to_f32<T>((uint16_t)v[i]) + ppmm::to_f32<T>((uint16_t)(v[i] >> 16));
+            sum = across_quarters(sum);
+            const uint32_t p0 = high_part(sum), p1 = high_part(sum - as_float(p0)), p2 = high_part(sum - as_float(p0) - as_float(p1));
+            const uint32_t p = h == 0 ? p0 : h == 1 ? p1 : h == 2 ? p2 : 0;
+            qsum[t][(kGroups + j) / 2] |= (kGroups + j) % 2 ? p : p >> 16;
+        }
+    }
+    // a one that brings out the column's scale, and one for its offset
+    u32x4 one_s = {0, 0, 0, 0}, one_b = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j)
+        if (h == 0 && mine == j) {
+            one_s[j / 2] = j % 2 ? 0x3f800000u : 0x3f80u;
+            one_b[(kGroups + j) / 2] = (kGroups + j) % 2 ? 0x3f800000u : 0x3f80u;
+        }
+    constexpr int kSums = kFew ? 1 : kGroups;       // sums of p b that a lane keeps
+    f32x4 o[kTiles][kChannelTiles] = {};
+    float z[kTiles][kSums] = {}, most[kTiles], sum[kTiles] = {};
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) most[t] = -INFINITY;
+
+    // ---- a tile's codes, scales and offsets, asked for one tile ahead ----
+    uint32_t kc[4][kGroups], vc[4][kGroups], kp[4][kParamWords], vp[4][kParamWords];
+    uint32_t bad = 0;                               // 16 keys in a page that is none
+    const auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
+        const uint32_t blocks = (uint32_t)c.page_size / 16, block0 = (uint32_t)(k0 / 16);
+        uint32_t at = block0 / blocks, in = block0 - at * blocks;
+        bad = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // a page behind the table or outside the pool: page 0 instead, and its keys do not count
+            int32_t page = at < (uint32_t)c.table_width ? c.table[(int64_t)b * c.table_width + at] : -1;
+            if (page < 0 || page >= c.pages) { bad |= 1u << i; page = 0; }
+            const uint8_t *base = c.pool + ((int64_t)page * c.kv_heads + rows.kv_head) * c.page_bytes();
+            const int slot = 16 * in;
+            __builtin_memcpy(kc[i], base + codes_at<D>(c, 0, slot) + lane % 16 * (D / 2) + h * 4 * kGroups, 4 * kGroups);
+            __builtin_memcpy(vc[i], base + codes_at<D>(c, 1, slot) + lane * 4 * kGroups, 4 * kGroups);
+            __builtin_memcpy(kp[i], base + params_at<D>(c, 0, slot) + col * 4 * kParamWords, 4 * kParamWords);
+            __builtin_memcpy(vp[i], base + params_at<D>(c, 1, slot) + col * 4 * kParamWords, 4 * kParamWords);
+            if (++in == blocks) { in = 0; ++at; }
+        }
+    };
+    const ppmm::Unpacker<T> unpack;
+    const ppmm::Unpacker<BF16> unpack_values;
+    uint8_t *shared = lds.values[wave];
+    int64_t k0 = begin + 64 * wave;
+    if (k0 < end) fetch(k0);
+    for (; k0 < end; k0 += 256) {
+        const uint32_t wrong = bad;
+        const bool whole = k0 + 64 <= clear && !wrong;
+        // ---- scores ----
+        f32x4 p[kTiles][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x4 params = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < kParamWords; ++w) params[w] = kp[i][w];
+            const f32x4 zero = {0, 0, 0, 0}, s = BF16::mma(params, one_s, zero);
+            u32x4 keys[kGroups];
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) keys[j] = unpack.template get<kKeyBit>(kc[i][j]);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                f32x4 score = BF16::mma(params, qsum[t], zero);
+                if constexpr (kFew) {
+                    f32x4 acc = zero;
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j) acc = T::mma(keys[j], qs[t][j], acc);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = fmaf(s[e], acc[e], score[e]);
+                        v += dpp<kRor8>(v);
+                        if constexpr (kGroups == 4) v += dpp<kRor4>(v);
+                        score[e] = v;
+                    }
+                } else {
+                    f32x4 acc[kGroups];
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j) acc[j] = T::mma(keys[j], qs[t][j], zero);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        score[e] = fmaf(dpp<quad_of(0, kGroups)>(s[e]), acc[0][e], score[e]);
+                        score[e] = fmaf(dpp<quad_of(1, kGroups)>(s[e]), acc[1][e], score[e]);
+                        if constexpr (kGroups == 4) {
+                            score[e] = fmaf(dpp<quad_of(2, 4)>(s[e]), acc[kGroups - 2][e], score[e]);
+                            score[e] = fmaf(dpp<quad_of(3, 4)>(s[e]), acc[kGroups - 1][e], score[e]);
+                        }
+                    }
+                }
+                p[t][i] = score * scale;
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t key = k0 + 16 * i + 4 * h;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key + e >= limit[t] || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
+                // values that do not count: whatever lies there, its scale and offset are zero
+                const bool none = k0 + 16 * i + col >= held || (wrong >> i & 1);
+#pragma unroll
+                for (int w = 0; w < kParamWords; ++w) vp[i][w] = none ? 0 : vp[i][w];
+            }
+        }
+        // Groups of values that read as NaN: their offset would spoil other groups and rows that do not attend to them (0 * NaN).  It is
+        // taken out, and the sums of the rows that do attend to them become NaN.
+        typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
+        v2u16 largest = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int w = kParamWords / 2; w < kParamWords; ++w)
+                largest = __builtin_elementwise_max(largest, __builtin_bit_cast(v2u16, vp[i][w] & 0x7fff7fffu));
+        if (__ballot(largest[0] >= 0x7f80 || largest[1] >= 0x7f80)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u32x4 flags = {0, 0, 0, 0};
+#pragma unroll
+                for (int w = kParamWords / 2; w < kParamWords; ++w) {
+                    const uint32_t v = vp[i][w], lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
+                    flags[w] = (lo ? 0x3f80u : 0) | (hi ? 0x3f800000u : 0);
+                    vp[i][w] = v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+                }
+                const f32x4 flag = BF16::mma(flags, one_b, f32x4{0, 0, 0, 0});
+                const auto poison = [&](int n, const f32x4 &f) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (f[e] != 0.0f && k0 + 16 * i + 4 * h + e < limit[t]) z[t][n] = NAN;
+                };
+                if constexpr (kFew) poison(0, flag);
+                else {
+                    const auto of = [&](auto index) __attribute__((always_inline)) {
+                        constexpr int ctrl = quad_of(decltype(index)::value, kGroups);
+                        poison(decltype(index)::value, f32x4{dpp<ctrl>(flag[0]), dpp<ctrl>(flag[1]), dpp<ctrl>(flag[2]), dpp<ctrl>(flag[3])});
+                    };
+                    of(std::integral_constant<int, 0>());
+                    of(std::integral_constant<int, 1>());
+                    if constexpr (kGroups == 4) {
+                        of(std::integral_constant<int, 2>());
+                        of(std::integral_constant<int, 3>());
+                    }
+                }
+            }
+        }
+        // ---- probabilities: the largest score counts from where it was unless it grew by more than 2^8 ----
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            float top = fmaxf(fmaxf(p[t][0][0], p[t][0][1]), fmaxf(p[t][0][2], p[t][0][3]));
+#pragma unroll
+            for (int i = 1; i < 4; ++i) top = fmaxf(top, fmaxf(fmaxf(p[t][i][0], p[t][i][1]), fmaxf(p[t][i][2], p[t][i][3])));
+            top = most_of_quarters(top);
+            const bool grew = top > most[t] + 8.0f || most[t] == -INFINITY;
+            if (__ballot(grew && top != -INFINITY)) {
+                const float now = grew ? fmaxf(top, most[t]) : most[t];
+                const float keep = most[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most[t] - now);
+                most[t] = now;
+                sum[t] *= keep;
+#pragma unroll
+                for (int n = 0; n < kSums; ++n) z[t][n] *= keep;
+#pragma unroll
+                for (int n = 0; n < kChannelTiles; ++n) o[t][n] *= keep;
+            }
+            const float from = most[t] == -INFINITY ? 0.0f : most[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[t][i][e] = __builtin_amdgcn_exp2f(p[t][i][e] - from);
+                    sum[t] += p[t][i][e];
+                }
+        }
+        // ---- values ----
+        f32x4 s[4], off[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x4 params = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < kParamWords; ++w) params[w] = vp[i][w];
+            s[i] = BF16::mma(params, one_s, f32x4{0, 0, 0, 0});
+            off[i] = BF16::mma(params, one_b, f32x4{0, 0, 0, 0});
+            __builtin_memcpy(__builtin_assume_aligned(shared + (16 * i + lane / 4) * kPitch + lane % 4 * 4 * kGroups, 4 * kGroups), vc[i], 4 * kGroups);
+        }
+        if (k0 + 256 < end) fetch(k0 + 256);
+        const uint8_t *from = shared + (16 * (col / 4) + 4 * h + col % 4) * kPitch;
+        const auto add_values = [&](int n, const u32x4 (&big)[kTiles][2], const u32x4 (&small)[kTiles][2]) __attribute__((always_inline)) {
+            typedef int v2i __attribute__((ext_vector_type(2)));
+            const v2i w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i *)(from + 8 * n));
+            const u32x4 v0 = unpack_values.get<0>((uint32_t)w[0]), v1 = unpack_values.get<0>((uint32_t)w[1]);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                o[t][n] = BF16::mma(v0, big[t][0], o[t][n]);
+                o[t][n] = BF16::mma(v1, big[t][1], o[t][n]);
+                o[t][n] = BF16::mma(v0, small[t][0], o[t][n]);
+                o[t][n] = BF16::mma(v1, small[t][1], o[t][n]);
+            }
+        };
+        // p times scale in two halves, and p times offset
+        const auto weigh = [&](int t, int n, const f32x4 (&sj)[4], const f32x4 (&bj)[4], u32x4 (&big)[2], u32x4 (&small)[2]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = p[t][2 * half][e] * sj[2 * half][e], y = p[t][2 * half + 1][e] * sj[2 * half + 1][e];
+                    big[half][e] = pack_high(x, y);
+                    small[half][e] = pack_bf16(x - as_float(high_part(x)), y - as_float(high_part(y)));
+                    z[t][n] = fmaf(p[t][2 * half][e], bj[2 * half][e], z[t][n]);
+                    z[t][n] = fmaf(p[t][2 * half + 1][e], bj[2 * half + 1][e], z[t][n]);
+                }
+        };
+        u32x4 big[kTiles][2], small[kTiles][2];
+        if constexpr (kFew) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) weigh(t, 0, s, off, big[t], small[t]);
+#pragma unroll
+            for (int n = 0; n < kChannelTiles; ++n) add_values(n, big, small);
+        } else {
+            const auto group = [&](auto index) __attribute__((always_inline)) {
+                constexpr int j = decltype(index)::value, ctrl = quad_of(j, kGroups);
+                f32x4 sj[4], bj[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sj[i][e] = dpp<ctrl>(s[i][e]);
+                        bj[i][e] = dpp<ctrl>(off[i][e]);
+                    }
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) weigh(t, j, sj, bj, big[t], small[t]);
+                add_values(2 * j, big, small);
+                add_values(2 * j + 1, big, small);
+            };
+            group(std::integral_constant<int, 0>());
+            group(std::integral_constant<int, 1>());
+            if constexpr (kGroups == 4) {
+                group(std::integral_constant<int, 2>());
+                group(std::integral_constant<int, 3>());
+            }
+        }
+    }
+
+    // ---- the four waves' parts together ----
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        sum[t] = across_quarters(sum[t]);
+#pragma unroll
+        for (int n = 0; n < kSums; ++n) z[t][n] = across_quarters(z[t][n]);
+        if (h == 0) {
+            stats[0][wave][t][col] = most[t];
+            stats[1][wave][t][col] = sum[t];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[0][w][t][col]);
+        const float keep = most[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most[t] - top);
+        if (t) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kChannelTiles; ++n)
+            if (!kFew || mine == n / 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lds.joined[wave][query][16 * n + 4 * h + e] = (o[t][n][e] + z[t][kFew ? 0 : n / 2]) * keep;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kQueries * D; i += 256) {
+            const int k = i / D, ch = i % D;
+            float m = -INFINITY, l = 0.0f, v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[0][w][t][k]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float mw = stats[0][w][t][k];
+                l += mw == -INFINITY ? 0.0f : stats[1][w][t][k] * __builtin_amdgcn_exp2f(mw - m);
+                v += lds.joined[w][k][ch];
+            }
+            const int64_t r = row0 + t * kQueries + k, n = rows.token(r);
+            if (r >= count || n < 0 || n >= tokens) continue;
+            const int head = rows.kv_head * rows.G + (int)(r % rows.G);
+            if (splits == 1) out[n * ots + head * ohs + ch] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : v / l);
+            else {
+                float *to = scratch + ((n * heads + head) * splits + split) * (D + 2);
+                to[ch] = v;
+                if (ch == 0) { to[D] = m; to[D + 1] = l; }
+            }
+        }
+    }
+}
+
+// Joins the splits of a row: one wave a row and head.
+template <class T, int D>
+__global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int32_t heads, uint16_t *out, int64_t ots, int64_t ohs, int32_t max_q, int32_t splits,
+                                                   const float *scratch)
+{
+    const int lane = threadIdx.x % 64;
+    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, n = row / heads;
+    if (n >= tokens) return;
     const int32_t b = c.sequence_of(n);
-    if (b < 0) return;
-    const int64_t first = c.starts[b], next = c.starts[b + 1];
-    if (n - first >= max_q) return;
-    int64_t len = c.lens[b];
-    const int64_t position = len - (next - n);
-    if (causal && position + 1 < len) len = position + 1;
-    if (len > c.capacity()) len = c.capacity();
-    float x[E], o[E] = {};
-    const int ch = threadIdx.x * E;
+    if (b < 0 || n - c.starts[b] >= max_q) return;
+    const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits);
+    const int used = held > part ? (int)((held + part - 1) / part) : 1;
+    const float *from = scratch + row * splits * (D + 2);
+    float m = -INFINITY, l = 0.0f, v[D / 64] = {};
+    for (int s = 0; s < used; ++s) m = fmaxf(m, from[s * (D + 2) + D]);
+    for (int s = 0; s < used; ++s) {
+        const float ms = from[s * (D + 2) + D], keep = ms == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms - m);
+        l = fmaf(keep, from[s * (D + 2) + D + 1], l);
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = ppmm::to_f32<T>(q[n * qts + qh * qhs + ch + e]);
-    float most = -INFINITY, sum = 0.0f;
-    const int j = ch / 32, h = ch / 8 % 4;
-    for (int64_t i = 0; i < len; ++i) {
-        const uint8_t *page = c.page_of(b, i, head);
-        if (!page) continue;
-        const int slot = (int)(i % c.page_size);
-        const uint32_t kw = *(const uint32_t *)(page + codes_at<D>(c, 0, slot) + 4 * ((D / 32) * h + j));
-        const uint32_t vw = *(const uint32_t *)(page + codes_at<D>(c, 1, slot) + 4 * (ch / 8));
-        const uint32_t kp = *(const uint32_t *)(page + params_at<D>(c, 0, slot) + 4 * j);
-        const uint32_t vp = *(const uint32_t *)(page + params_at<D>(c, 1, slot) + 4 * j);
-        float dot = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            dot = fmaf(x[e], fmaf(ppmm::to_f32<BF16>((uint16_t)kp), 16.0f + (float)(kw >> (4 * (ch % 8 + e)) & 15), ppmm::to_f32<BF16>((uint16_t)(kp >> 16))), dot);
-#pragma unroll
-        for (int step = 32; step; step /= 2) dot += __shfl_xor(dot, step);
-        const float score = dot * scale;
-        const float top = fmaxf(most, score);
-        const float keep = most == -INFINITY ? 0.0f : expf(most - top), p = top == -INFINITY ? 0.0f : expf(score - top);
-        sum = fmaf(sum, keep, p);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            o[e] = fmaf(o[e], keep, p * fmaf(ppmm::to_f32<BF16>((uint16_t)vp), 16.0f + (float)(vw >> (4 * (ch % 8 + e)) & 15), ppmm::to_f32<BF16>((uint16_t)(vp >> 16))));
-        most = top;
+        for (int e = 0; e < D / 64; ++e) v[e] = fmaf(keep, from[s * (D + 2) + lane * (D / 64) + e], v[e]);
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[n * ots + qh * ohs + ch + e] = ppmm::from_f32<T>(sum == 0.0f ? 0.0f : o[e] / sum);
+    for (int e = 0; e < D / 64; ++e)
+        out[n * ots + row % heads * ohs + lane * (D / 64) + e] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : v[e] / l);
 }
 
 Cache device_cache(const ppkv_cache *c, const ppkv_batch *b)
@@ -237,8 +626,9 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
 size_t ppkv_attention_scratch_bytes(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, int32_t heads, int32_t max_q,
                                     int64_t max_len, int32_t device)
 {
-    (void)cache; (void)batch; (void)tokens; (void)heads; (void)max_q; (void)max_len; (void)device;
-    return 0;
+    if (ppmm_host::check_attention(cache, batch, tokens, PPMM_BF16, heads, max_q, max_len, device) != PCMM_OK) return 0;
+    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len);
+    return d.splits == 1 ? 0 : (size_t)tokens * heads * d.splits * (cache->head_dim + 2) * sizeof(float);
 }
 
 pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, ppmm_type type, int32_t heads,
@@ -251,16 +641,36 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
     if (!ppmm_host::read_strides_ok(qts, qhs) || !ppmm_host::rows_apart(tokens, heads, D, ots, ohs)) return PCMM_EINVAL;
     if (tokens == 0 || max_q == 0) return PCMM_OK;
     if (!q_dev || !out_dev || q_dev == out_dev) return PCMM_EINVAL;
-    if (scratch_bytes < ppkv_attention_scratch_bytes(cache, batch, tokens, heads, max_q, max_len, device)) return PCMM_EINVAL;
-    (void)scratch;
-    const uint32_t blocks = blocks_for(tokens * heads * 64, 64);
-    if (!blocks) return PCMM_EUNSUPPORTED;
+    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len);
+    if (d.splits > 1 && (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ppkv_attention_scratch_bytes(cache, batch, tokens, heads, max_q, max_len, device)))
+        return PCMM_EINVAL;
+    const int64_t join_blocks = (tokens * heads + 3) / 4;
+    if (d.row_sets * d.splits > 0xffffff || join_blocks > 0xffffff) return PCMM_EUNSUPPORTED;      // no launch of 2^32 threads in one direction
     pcmm_hip_util::DevGuard dg(device);
     if (!dg.ok) return PCMM_EDEVICE;
-    auto kernel = type == PPMM_BF16 ? (D == 64 ? attention_kernel<BF16, 64> : attention_kernel<BF16, 128>)
-                                    : (D == 64 ? attention_kernel<FP16, 64> : attention_kernel<FP16, 128>);
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64), 0, (hipStream_t)stream, device_cache(cache, batch), tokens, heads, (const uint16_t *)q_dev,
-                       qts, qhs, (uint16_t *)out_dev, ots, ohs, scale, causal, max_q);
+    const Cache c = device_cache(cache, batch);
+    const float scale2 = scale * 1.44269504f;
+    const dim3 grid((unsigned)(d.row_sets * d.splits), (unsigned)cache->kv_heads, (unsigned)batch->batch);
+    const auto launch = [&](auto kernel, auto join) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, c, tokens, heads, (const uint16_t *)q_dev, qts, qhs, (uint16_t *)out_dev, ots, ohs,
+                           scale2, causal, max_q, (int32_t)d.splits, (float *)scratch);
+        if (d.splits > 1)
+            hipLaunchKernelGGL(join, dim3((unsigned)join_blocks), dim3(256), 0, (hipStream_t)stream, c, tokens, heads, (uint16_t *)out_dev, ots, ohs, max_q,
+                               (int32_t)d.splits, (const float *)scratch);
+    };
+    const auto by_shape = [&](auto tag) {
+        using T = decltype(tag);
+        if (D == 128) {
+            if (d.few && d.tiles == 1) launch(attention_kernel<T, 128, 1, true>, join_kernel<T, 128>);
+            else if (d.few) launch(attention_kernel<T, 128, 2, true>, join_kernel<T, 128>);
+            else launch(attention_kernel<T, 128, 2, false>, join_kernel<T, 128>);
+        } else {
+            if (d.few) launch(attention_kernel<T, 64, 1, true>, join_kernel<T, 64>);
+            else launch(attention_kernel<T, 64, 2, false>, join_kernel<T, 64>);
+        }
+    };
+    if (type == PPMM_BF16) by_shape(BF16());
+    else by_shape(FP16());
     return hipGetLastError() == hipSuccess ? PCMM_OK : PCMM_EDEVICE;
 }
 

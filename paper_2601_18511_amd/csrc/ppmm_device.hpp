@@ -45,14 +45,18 @@ __device__ inline uint32_t rotate_right(uint32_t v, int by) { return __builtin_a
 template <class T> struct Unpacker {
     uint32_t mask, sixteen;
     __device__ inline Unpacker() : mask(0x000F000Fu << T::kCodeBit), sixteen(T::kSixteen) { asm("" : "+s"(mask), "+v"(sixteen)); }
-    __device__ inline u32x4 operator()(uint32_t w) const
+    // kFirst: the bit at which nibble 0 lies
+    template <int kFirst = T::kCodeBit> __device__ inline u32x4 get(uint32_t w) const
     {
         u32x4 v;
-        v[0] = (w & mask) | sixteen;
 #pragma unroll
-        for (int i = 1; i < 4; ++i) v[i] = (rotate_right(w, 4 * i) & mask) | sixteen;
+        for (int i = 0; i < 4; ++i) {
+            const int by = (4 * i + kFirst - T::kCodeBit + 32) % 32;
+            v[i] = ((by ? rotate_right(w, by) : w) & mask) | sixteen;
+        }
         return v;
     }
+    __device__ inline u32x4 operator()(uint32_t w) const { return get(w); }
 };
 
 template <class T> __device__ inline float to_f32(uint16_t bits) { return (float)__builtin_bit_cast(typename T::type, bits); }
@@ -66,7 +70,7 @@ struct Cache {
     const int32_t *starts, *lens, *table;
     int32_t batch, table_width;
 
-    // bytes of one page of one head: [codes of keys][codes of values][(s, b) of keys][(s, b) of values]
+    // bytes of one page of one head: [codes of keys][codes of values][scales and offsets of keys][of values]
     __device__ int64_t page_bytes() const { return (int64_t)page_size * (head_dim + head_dim / 4); }
     __device__ int64_t capacity() const { return (int64_t)table_width * page_size; }
 

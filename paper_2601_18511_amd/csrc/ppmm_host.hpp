@@ -92,6 +92,31 @@ inline pcmm_status check_attention(const ppkv_cache *c, const ppkv_batch *b, int
     return PCMM_OK;
 }
 
+// How attention is divided among work-groups: `tiles` tiles of columns each, `splits` of the keys.
+struct Division {
+    bool few;           // a column is a pair of group and query
+    int tiles;
+    int64_t row_sets, splits;
+};
+
+inline Division divide(const ppkv_cache &c, const ppkv_batch &b, int32_t heads, int32_t max_q, int64_t max_len)
+{
+    const int64_t rows = (int64_t)max_q * (heads / c.kv_heads), per_tile = 16 / (c.head_dim / 32), capacity = (int64_t)b.table_width * c.page_size;
+    const int64_t longest = max_len > 0 && max_len < capacity ? max_len : capacity;
+    Division d;
+    const int most = c.head_dim == 128 ? 2 : 1;     // tiles of few queries that a work-group takes
+    d.few = rows <= most * per_tile;
+    d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : 2;
+    const int64_t set = d.tiles * (d.few ? per_tile : 16);
+    d.row_sets = rows > 0 ? (rows + set - 1) / set : 0;
+    // enough work-groups for the chip, none with less than a round of its four waves (256 keys)
+    const int64_t groups = d.row_sets * c.kv_heads * b.batch, want = groups > 0 ? (1024 + groups - 1) / groups : 1, rounds = (longest + 255) / 256;
+    d.splits = want < rounds ? want : rounds;
+    if (d.splits < 1) d.splits = 1;
+    if (d.splits > 64) d.splits = 64;
+    return d;
+}
+
 }  // namespace ppmm_host
 
 #endif  // PPMM_HOST_HPP
