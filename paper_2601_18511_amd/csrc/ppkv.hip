@@ -164,8 +164,17 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
 // The four waves of a work-group share out the tiles of its keys and join at the end; where there are few rows, several
 // work-groups share out the keys of a row and a second kernel joins them.
 
+// over the four lanes of a column
 __device__ inline float across_quarters(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
-__device__ inline float most_of_quarters(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ inline float most_of_quarters(float v)
+{
+    const uint32_t a = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);        // the even rows of lanes twice, and the odd ones
+    v = fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    const uint32_t c = __builtin_bit_cast(uint32_t, v);
+    const auto t = __builtin_amdgcn_permlane32_swap(c, c, false, false);        // the lower half twice, and the upper one
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)t[0]), __builtin_bit_cast(float, (uint32_t)t[1]));
+}
 template <int kCtrl> __device__ inline float dpp(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
@@ -184,11 +193,11 @@ struct Rows {
     int32_t G, kv_head;
     bool causal;
     __device__ inline int64_t token(int64_t r) const { return first + r / G; }
-    __device__ inline int64_t limit(int64_t r) const        // keys that row r attends to
+    __device__ inline int32_t limit(int64_t r) const        // keys that row r attends to
     {
         const int64_t held = length < capacity ? length : capacity, own = length - (next - token(r)) + 1;
         const int64_t n = causal && own < held ? own : held;
-        return n > 0 ? n : 0;
+        return n > 0 ? (int32_t)n : 0;                      // the capacity is below 2^31
     }
 };
 
@@ -201,7 +210,6 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 {
     constexpr int kGroups = D / 32, kChannelTiles = D / 16, kQueries = kFew ? 16 / kGroups : 16, kRows = kQueries * kTiles;
     constexpr int kPitch = D / 2 + 16;              // bytes of a token's values in LDS
-    constexpr int kParamWords = D / 32;             // 32-bit words of a token's scales and offsets
     __shared__ union {                              // the waves' values, and after the last key their results
         __attribute__((aligned(16))) uint8_t values[4][64 * kPitch];
         float joined[4][kQueries][D + 4];
@@ -213,18 +221,19 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     const int64_t news = rows.next - rows.first < max_q ? rows.next - rows.first : max_q, count = news * rows.G;
     const int64_t row0 = (int64_t)(blockIdx.x / splits) * kRows;
     if (row0 >= count) return;
-    const int64_t held = rows.length < rows.capacity ? rows.length : rows.capacity, part = split_size(held, splits);
+    const int32_t held = (int32_t)(rows.length < rows.capacity ? rows.length : rows.capacity);
+    const int64_t part = split_size(held, splits);
     const int64_t begin = split * part;
     if (split > 0 && begin >= held) return;
     const int64_t last = row0 + kRows < count ? row0 + kRows - 1 : count - 1;
-    int64_t end = rows.limit(last) < begin + part ? rows.limit(last) : begin + part;      // behind the keys of any row
-    const int64_t clear = rows.limit(row0);         // keys in front of this belong to every row
+    const int32_t end = rows.limit(last) < begin + part ? rows.limit(last) : (int32_t)(begin + part);      // behind the keys of any row
+    const int32_t clear = rows.limit(row0);         // keys in front of this belong to every row
 
     const int mine = kFew ? col / kQueries : col % kGroups;                  // the group whose scale this column brings out
     const int query = kFew ? col % kQueries : col;
     // the column's queries as the second operand, and its sums in three parts, one a quarter of the lanes
     u32x4 qs[kTiles][kGroups], qsum[kTiles];
-    int64_t limit[kTiles];
+    int32_t limit[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         const int64_t r = row0 + t * kQueries + query, n = rows.token(r);
@@ -259,42 +268,59 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) most[t] = -INFINITY;
 
-    // ---- a tile's codes, scales and offsets, asked for one tile ahead ----
-    uint32_t kc[4][kGroups], vc[4][kGroups], kp[4][kParamWords], vp[4][kParamWords];
+    // ---- a tile's codes, scales and offsets are asked for one tile ahead, its page numbers two ----
+    typedef uint32_t Words __attribute__((ext_vector_type(kGroups)));       // a lane's codes, and a token's scales and offsets
+    Words kc[4], vc[4], kp[4], vp[4];
     uint32_t bad = 0;                               // 16 keys in a page that is none
-    const auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
-        const uint32_t blocks = (uint32_t)c.page_size / 16, block0 = (uint32_t)(k0 / 16);
-        uint32_t at = block0 / blocks, in = block0 - at * blocks;
-        bad = 0;
+    int32_t page_ahead = -1;                        // of 16 keys each: lane l has the tile's part l % 4
+    uint32_t slot_ahead = 0;
+    const uint32_t page_blocks = (uint32_t)c.page_size / 16;
+    const int64_t value_codes = (int64_t)c.page_size * (D / 2), value_params = (int64_t)c.page_size * (D / 8), params_after = (int64_t)c.page_size * D;
+    const auto look_ahead = [&](int32_t k0) __attribute__((always_inline)) {
+        const uint32_t block = (uint32_t)k0 / 16 + lane % 4, at = block / page_blocks;
+        slot_ahead = (block - at * page_blocks) * 16;
+        page_ahead = -1;
+        if (at < (uint32_t)c.table_width) page_ahead = c.table[(int64_t)b * c.table_width + at];
+    };
+    const auto fetch = [&]() __attribute__((always_inline)) {
+        // a page behind the table or outside the pool: page 0 instead, and its keys do not count
+        const bool none = page_ahead < 0 || page_ahead >= c.pages;
+        bad = (uint32_t)__ballot(none) & 15;
+        const uint64_t page = (uint64_t)(none ? 0 : page_ahead) * c.kv_heads + rows.kv_head;
+        const uint64_t base = (uint64_t)c.pool + page * (uint64_t)c.page_bytes();
+        const uint64_t codes = base + slot_ahead * (D / 2), params = base + params_after + slot_ahead * (D / 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            // a page behind the table or outside the pool: page 0 instead, and its keys do not count
-            int32_t page = at < (uint32_t)c.table_width ? c.table[(int64_t)b * c.table_width + at] : -1;
-            if (page < 0 || page >= c.pages) { bad |= 1u << i; page = 0; }
-            const uint8_t *base = c.pool + ((int64_t)page * c.kv_heads + rows.kv_head) * c.page_bytes();
-            const int slot = 16 * in;
-            __builtin_memcpy(kc[i], base + codes_at<D>(c, 0, slot) + lane % 16 * (D / 2) + h * 4 * kGroups, 4 * kGroups);
-            __builtin_memcpy(vc[i], base + codes_at<D>(c, 1, slot) + lane * 4 * kGroups, 4 * kGroups);
-            __builtin_memcpy(kp[i], base + params_at<D>(c, 0, slot) + col * 4 * kParamWords, 4 * kParamWords);
-            __builtin_memcpy(vp[i], base + params_at<D>(c, 1, slot) + col * 4 * kParamWords, 4 * kParamWords);
-            if (++in == blocks) { in = 0; ++at; }
+            const auto of_lane = [&](uint64_t v) __attribute__((always_inline)) {
+                return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i));
+            };
+            const uint8_t *k = of_lane(codes), *s = of_lane(params);
+            kc[i] = ((const Words *)k)[col * 4 + h];
+            kp[i] = ((const Words *)s)[col];
+            vc[i] = ((const Words *)(k + value_codes))[lane];
+            vp[i] = ((const Words *)(s + value_params))[col];
         }
     };
     const ppmm::Unpacker<T> unpack;
     const ppmm::Unpacker<BF16> unpack_values;
     uint8_t *shared = lds.values[wave];
-    int64_t k0 = begin + 64 * wave;
-    if (k0 < end) fetch(k0);
-    for (; k0 < end; k0 += 256) {
+    int32_t k0 = (int32_t)begin + 64 * wave;        // lengths are below 2^31, and a tile ends behind them by 320 at the most
+    if (k0 < end) {
+        look_ahead(k0);
+        fetch();
+        if (k0 < end - 256) look_ahead(k0 + 256);
+    }
+    for (; k0 < end; k0 = k0 < end - 256 ? k0 + 256 : end) {
         const uint32_t wrong = bad;
-        const bool whole = k0 + 64 <= clear && !wrong;
+        const bool whole = k0 <= clear - 64 && !wrong;
         // ---- scores ----
         f32x4 p[kTiles][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u32x4 params = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < kParamWords; ++w) params[w] = kp[i][w];
+            for (int w = 0; w < kGroups; ++w) params[w] = kp[i][w];
             const f32x4 zero = {0, 0, 0, 0}, s = BF16::mma(params, one_s, zero);
             u32x4 keys[kGroups];
 #pragma unroll
@@ -333,16 +359,16 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t key = k0 + 16 * i + 4 * h;
+                const int32_t key = 16 * i + 4 * h;
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (key + e >= limit[t] || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
+                        if (key + e >= limit[t] - k0 || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
                 // values that do not count: whatever lies there, its scale and offset are zero
-                const bool none = k0 + 16 * i + col >= held || (wrong >> i & 1);
+                const bool none = 16 * i + col >= held - k0 || (wrong >> i & 1);
 #pragma unroll
-                for (int w = 0; w < kParamWords; ++w) vp[i][w] = none ? 0 : vp[i][w];
+                for (int w = 0; w < kGroups; ++w) vp[i][w] = none ? 0 : vp[i][w];
             }
         }
         // Groups of values that read as NaN: their offset would spoil other groups and rows that do not attend to them (0 * NaN).  It is
@@ -352,14 +378,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int w = kParamWords / 2; w < kParamWords; ++w)
+            for (int w = kGroups / 2; w < kGroups; ++w)
                 largest = __builtin_elementwise_max(largest, __builtin_bit_cast(v2u16, vp[i][w] & 0x7fff7fffu));
         if (__ballot(largest[0] >= 0x7f80 || largest[1] >= 0x7f80)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 u32x4 flags = {0, 0, 0, 0};
 #pragma unroll
-                for (int w = kParamWords / 2; w < kParamWords; ++w) {
+                for (int w = kGroups / 2; w < kGroups; ++w) {
                     const uint32_t v = vp[i][w], lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
                     flags[w] = (lo ? 0x3f80u : 0) | (hi ? 0x3f800000u : 0);
                     vp[i][w] = v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
@@ -370,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (f[e] != 0.0f && k0 + 16 * i + 4 * h + e < limit[t]) z[t][n] = NAN;
+                            if (f[e] != 0.0f && 16 * i + 4 * h + e < limit[t] - k0) z[t][n] = NAN;
                 };
                 if constexpr (kFew) poison(0, flag);
                 else {
@@ -420,12 +446,15 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         for (int i = 0; i < 4; ++i) {
             u32x4 params = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < kParamWords; ++w) params[w] = vp[i][w];
+            for (int w = 0; w < kGroups; ++w) params[w] = vp[i][w];
             s[i] = BF16::mma(params, one_s, f32x4{0, 0, 0, 0});
             off[i] = BF16::mma(params, one_b, f32x4{0, 0, 0, 0});
-            __builtin_memcpy(__builtin_assume_aligned(shared + (16 * i + lane / 4) * kPitch + lane % 4 * 4 * kGroups, 4 * kGroups), vc[i], 4 * kGroups);
+            *(Words *)(shared + (16 * i + lane / 4) * kPitch + lane % 4 * 4 * kGroups) = vc[i];
         }
-        if (k0 + 256 < end) fetch(k0 + 256);
+        if (k0 < end - 256) {
+            fetch();
+            if (k0 < end - 512) look_ahead(k0 + 512);
+        }
         const uint8_t *from = shared + (16 * (col / 4) + 4 * h + col % 4) * kPitch;
         const auto add_values = [&](int n, const u32x4 (&big)[kTiles][2], const u32x4 (&small)[kTiles][2]) __attribute__((always_inline)) {
             typedef int v2i __attribute__((ext_vector_type(2)));
@@ -544,14 +573,21 @@ __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int3
     if (b < 0 || n - c.starts[b] >= max_q) return;
     const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits);
     const int used = held > part ? (int)((held + part - 1) / part) : 1;
+    // a lane looks at one split's maximum and sum (there are at most 64), then all lanes take the weighted rows together
     const float *from = scratch + row * splits * (D + 2);
-    float m = -INFINITY, l = 0.0f, v[D / 64] = {};
-    for (int s = 0; s < used; ++s) m = fmaxf(m, from[s * (D + 2) + D]);
-    for (int s = 0; s < used; ++s) {
-        const float ms = from[s * (D + 2) + D], keep = ms == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms - m);
-        l = fmaf(keep, from[s * (D + 2) + D + 1], l);
+    const bool live = lane < used;
+    const float mine = live ? from[lane * (D + 2) + D] : -INFINITY, mine_sum = live ? from[lane * (D + 2) + D + 1] : 0.0f;
+    float m = mine;
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[e] = fmaf(keep, from[s * (D + 2) + lane * (D / 64) + e], v[e]);
+    for (int step = 32; step; step /= 2) m = fmaxf(m, __shfl_xor(m, step));
+    const float keep = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - m);
+    float l = keep * mine_sum, v[D / 64] = {};
+#pragma unroll
+    for (int step = 32; step; step /= 2) l += __shfl_xor(l, step);
+    for (int s = 0; s < used; ++s) {
+        const float w = __shfl(keep, s);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) v[e] = fmaf(w, from[s * (D + 2) + lane * (D / 64) + e], v[e]);
     }
 #pragma unroll
     for (int e = 0; e < D / 64; ++e)
@@ -663,7 +699,7 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
         if (D == 128) {
             if (d.few && d.tiles == 1) launch(attention_kernel<T, 128, 1, true>, join_kernel<T, 128>);
             else if (d.few) launch(attention_kernel<T, 128, 2, true>, join_kernel<T, 128>);
-            else launch(attention_kernel<T, 128, 2, false>, join_kernel<T, 128>);
+            else launch(attention_kernel<T, 128, 1, false>, join_kernel<T, 128>);
         } else {
             if (d.few) launch(attention_kernel<T, 64, 1, true>, join_kernel<T, 64>);
             else launch(attention_kernel<T, 64, 2, false>, join_kernel<T, 64>);

@@ -106,11 +106,13 @@ inline Division divide(const ppkv_cache &c, const ppkv_batch &b, int32_t heads, 
     Division d;
     const int most = c.head_dim == 128 ? 2 : 1;     // tiles of few queries that a work-group takes
     d.few = rows <= most * per_tile;
-    d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : 2;
+    d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : most == 2 ? 1 : 2;
     const int64_t set = d.tiles * (d.few ? per_tile : 16);
     d.row_sets = rows > 0 ? (rows + set - 1) / set : 0;
-    // enough work-groups for the chip, none with less than a round of its four waves (256 keys)
-    const int64_t groups = d.row_sets * c.kv_heads * b.batch, want = groups > 0 ? (1024 + groups - 1) / groups : 1, rounds = (longest + 255) / 256;
+    // Enough work-groups for the chip, none with less than a round of its four waves (256 keys).  While rows are few, also no more than
+    // four rounds: where lengths differ, the longest sequences would be left over (32 requests of 50 to 16384 tokens).
+    const int64_t groups = d.row_sets * c.kv_heads * b.batch, rounds = (longest + 255) / 256;
+    const int64_t fill = groups > 0 ? (1024 + groups - 1) / groups : 1, even = groups < 4096 ? (rounds + 3) / 4 : 1, want = fill > even ? fill : even;
     d.splits = want < rounds ? want : rounds;
     if (d.splits < 1) d.splits = 1;
     if (d.splits > 64) d.splits = 64;
