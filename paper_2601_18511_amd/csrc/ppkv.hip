@@ -190,10 +190,11 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) { return ppmm::from_f32
 // Rows of one sequence and K/V head: row r is new token r / G, head G * kv_head + r % G.
 struct Rows {
     int64_t first, next, tokens, length, capacity;
-    int32_t G, kv_head;
+    uint32_t G;
+    int32_t kv_head;
     bool causal;
-    __device__ inline int64_t token(int64_t r) const { return first + r / G; }
-    __device__ inline int32_t limit(int64_t r) const        // keys that row r attends to
+    __device__ inline int64_t token(uint32_t r) const { return first + r / G; }
+    __device__ inline int32_t limit(uint32_t r) const        // keys that row r attends to
     {
         const int64_t held = length < capacity ? length : capacity, own = length - (next - token(r)) + 1;
         const int64_t n = causal && own < held ? own : held;
@@ -201,12 +202,16 @@ struct Rows {
     }
 };
 
-// The keys of one split: `of` of them, whole rounds of the four waves.
-__device__ inline int64_t split_size(int64_t length, int splits) { return (((length > 0 ? length : 0) + splits - 1) / splits + 255) / 256 * 256; }
+// Keys of one split: a multiple of unit, which is whole rounds of the four waves.
+__device__ inline int64_t split_size(int64_t length, int splits, int unit)
+{
+    const uint32_t n = length > 0 ? (uint32_t)length : 0;
+    return (int64_t)((n + splits - 1) / splits + unit - 1) / unit * unit;
+}
 
 template <class T, int D, int kTiles, bool kFew>
 __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t tokens, int32_t heads, const uint16_t *q, int64_t qts, int64_t qhs, uint16_t *out,
-                                                           int64_t ots, int64_t ohs, float scale, int32_t causal, int32_t max_q, int32_t splits, float *scratch)
+                                                           int64_t ots, int64_t ohs, float scale, int32_t causal, int32_t max_q, uint32_t row_sets, int32_t splits, int32_t unit, float *scratch)
 {
     constexpr int kGroups = D / 32, kChannelTiles = D / 16, kQueries = kFew ? 16 / kGroups : 16, kRows = kQueries * kTiles;
     constexpr int kPitch = D / 2 + 16;              // bytes of a token's values in LDS
@@ -216,16 +221,25 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     } lds;
     __shared__ float stats[2][4][kTiles][16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
-    const int32_t b = blockIdx.z, split = blockIdx.x % splits;
-    Rows rows{c.starts[b], c.starts[b + 1], tokens, c.lens[b], c.capacity(), heads / c.kv_heads, (int32_t)blockIdx.y, causal != 0};
-    const int64_t news = rows.next - rows.first < max_q ? rows.next - rows.first : max_q, count = news * rows.G;
-    const int64_t row0 = (int64_t)(blockIdx.x / splits) * kRows;
+    // Heads first, then sequences, then sets of rows from the last one on (they attend to the most), then splits: neighbouring
+    // work-groups go to different XCDs, and what neighbours have to do should be alike.
+    uint32_t id = blockIdx.x;
+    const int32_t kv_head = id % c.kv_heads;
+    id /= c.kv_heads;
+    const int32_t b = id % c.batch;
+    id /= c.batch;
+    const uint32_t set = row_sets - 1 - id % row_sets;
+    const int32_t split = id / row_sets;
+    Rows rows{c.starts[b], c.starts[b + 1], tokens, c.lens[b], c.capacity(), (uint32_t)(heads / c.kv_heads), kv_head, causal != 0};
+    const int64_t news = rows.next - rows.first < max_q ? rows.next - rows.first : max_q;
+    if (news <= 0) return;
+    const uint32_t count = (uint32_t)news * rows.G, row0 = set * kRows;       // max_q * G is below 2^31
     if (row0 >= count) return;
     const int32_t held = (int32_t)(rows.length < rows.capacity ? rows.length : rows.capacity);
-    const int64_t part = split_size(held, splits);
+    const int64_t part = split_size(held, splits, unit);
     const int64_t begin = split * part;
     if (split > 0 && begin >= held) return;
-    const int64_t last = row0 + kRows < count ? row0 + kRows - 1 : count - 1;
+    const uint32_t last = row0 + kRows < count ? row0 + kRows - 1 : count - 1;
     const int32_t end = rows.limit(last) < begin + part ? rows.limit(last) : (int32_t)(begin + part);      // behind the keys of any row
     const int32_t clear = rows.limit(row0);         // keys in front of this belong to every row
 
@@ -236,7 +250,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     int32_t limit[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-        const int64_t r = row0 + t * kQueries + query, n = rows.token(r);
+        const uint32_t r = row0 + t * kQueries + query;
+        const int64_t n = rows.token(r);
         const bool live = r < count && n >= 0 && n < tokens;
         limit[t] = live ? rows.limit(r) : 0;
         qsum[t] = u32x4{0, 0, 0, 0};
@@ -548,7 +563,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                 l += mw == -INFINITY ? 0.0f : stats[1][w][t][k] * __builtin_amdgcn_exp2f(mw - m);
                 v += lds.joined[w][k][ch];
             }
-            const int64_t r = row0 + t * kQueries + k, n = rows.token(r);
+            const uint32_t r = row0 + t * kQueries + k;
+            const int64_t n = rows.token(r);
             if (r >= count || n < 0 || n >= tokens) continue;
             const int head = rows.kv_head * rows.G + (int)(r % rows.G);
             if (splits == 1) out[n * ots + head * ohs + ch] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : v / l);
@@ -564,14 +580,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 // Joins the splits of a row: one wave a row and head.
 template <class T, int D>
 __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int32_t heads, uint16_t *out, int64_t ots, int64_t ohs, int32_t max_q, int32_t splits,
-                                                   const float *scratch)
+                                                   int32_t unit, const float *scratch)
 {
     const int lane = threadIdx.x % 64;
     const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, n = row / heads;
     if (n >= tokens) return;
     const int32_t b = c.sequence_of(n);
     if (b < 0 || n - c.starts[b] >= max_q) return;
-    const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits);
+    const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits, unit);
     const int used = held > part ? (int)((held + part - 1) / part) : 1;
     // a lane looks at one split's maximum and sum (there are at most 64), then all lanes take the weighted rows together
     const float *from = scratch + row * splits * (D + 2);
@@ -681,18 +697,19 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
     if (d.splits > 1 && (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ppkv_attention_scratch_bytes(cache, batch, tokens, heads, max_q, max_len, device)))
         return PCMM_EINVAL;
     const int64_t join_blocks = (tokens * heads + 3) / 4;
-    if (d.row_sets * d.splits > 0xffffff || join_blocks > 0xffffff) return PCMM_EUNSUPPORTED;      // no launch of 2^32 threads in one direction
+    const int64_t blocks = d.row_sets * d.splits * cache->kv_heads;                               // of one sequence
+    if (blocks > 0xffffff / batch->batch || join_blocks > 0xffffff) return PCMM_EUNSUPPORTED;     // no launch of 2^32 threads
     pcmm_hip_util::DevGuard dg(device);
     if (!dg.ok) return PCMM_EDEVICE;
     const Cache c = device_cache(cache, batch);
     const float scale2 = scale * 1.44269504f;
-    const dim3 grid((unsigned)(d.row_sets * d.splits), (unsigned)cache->kv_heads, (unsigned)batch->batch);
+    const dim3 grid((unsigned)(blocks * batch->batch));
     const auto launch = [&](auto kernel, auto join) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, c, tokens, heads, (const uint16_t *)q_dev, qts, qhs, (uint16_t *)out_dev, ots, ohs,
-                           scale2, causal, max_q, (int32_t)d.splits, (float *)scratch);
+                           scale2, causal, max_q, (uint32_t)d.row_sets, (int32_t)d.splits, d.unit, (float *)scratch);
         if (d.splits > 1)
             hipLaunchKernelGGL(join, dim3((unsigned)join_blocks), dim3(256), 0, (hipStream_t)stream, c, tokens, heads, (uint16_t *)out_dev, ots, ohs, max_q,
-                               (int32_t)d.splits, (const float *)scratch);
+                               (int32_t)d.splits, d.unit, (const float *)scratch);
     };
     const auto by_shape = [&](auto tag) {
         using T = decltype(tag);

@@ -89,6 +89,7 @@ inline pcmm_status check_attention(const ppkv_cache *c, const ppkv_batch *b, int
     if (rc != PCMM_OK) return rc;
     if ((type != PPMM_BF16 && type != PPMM_FP16) || max_q < 0 || max_len < 0) return PCMM_EINVAL;
     if (heads <= 0 || heads % c->kv_heads != 0 || heads / c->kv_heads > 65536) return PCMM_EINVAL;
+    if ((int64_t)max_q * (heads / c->kv_heads) > 0x7fffffff - 64) return PCMM_EUNSUPPORTED;      // rows of a sequence count in 32 bits
     return PCMM_OK;
 }
 
@@ -97,6 +98,7 @@ struct Division {
     bool few;           // a column is a pair of group and query
     int tiles;
     int64_t row_sets, splits;
+    int32_t unit;       // a split's keys are a multiple of this
 };
 
 inline Division divide(const ppkv_cache &c, const ppkv_batch &b, int32_t heads, int32_t max_q, int64_t max_len)
@@ -109,11 +111,14 @@ inline Division divide(const ppkv_cache &c, const ppkv_batch &b, int32_t heads, 
     d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : most == 2 ? 1 : 2;
     const int64_t set = d.tiles * (d.few ? per_tile : 16);
     d.row_sets = rows > 0 ? (rows + set - 1) / set : 0;
-    // Enough work-groups for the chip, none with less than a round of its four waves (256 keys).  While rows are few, also no more than
-    // four rounds: where lengths differ, the longest sequences would be left over (32 requests of 50 to 16384 tokens).
+    // Enough work-groups for the chip, none with less than a round of its four waves (256 keys).  While rows are few, also no split with
+    // more than four rounds, and none with fewer unless the chip needs them: lengths differ, and starting and joining cost a
+    // work-group as much as two rounds.
     const int64_t groups = d.row_sets * c.kv_heads * b.batch, rounds = (longest + 255) / 256;
-    const int64_t fill = groups > 0 ? (1024 + groups - 1) / groups : 1, even = groups < 4096 ? (rounds + 3) / 4 : 1, want = fill > even ? fill : even;
-    d.splits = want < rounds ? want : rounds;
+    const int64_t fill = groups > 0 ? (1024 + groups - 1) / groups : 1, even = groups < 4096 ? (rounds + 3) / 4 : 1;
+    d.unit = groups >= 256 ? 1024 : groups >= 128 ? 512 : 256;
+    d.splits = fill > even ? fill : even;
+    if (d.splits > (longest + d.unit - 1) / d.unit) d.splits = (longest + d.unit - 1) / d.unit;
     if (d.splits < 1) d.splits = 1;
     if (d.splits > 64) d.splits = 64;
     return d;
