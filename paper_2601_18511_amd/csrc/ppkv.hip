@@ -187,6 +187,21 @@ __device__ inline float as_float(uint32_t v) { return __builtin_bit_cast(float, 
 __device__ inline uint32_t pack_high(float lo, float hi) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u); }
 __device__ inline uint32_t pack_bf16(float lo, float hi) { return ppmm::from_f32<BF16>(lo) | (uint32_t)ppmm::from_f32<BF16>(hi) << 16; }
 
+// 64 lanes' 16 or 4 bytes from memory to neighbouring places in LDS, without a register in between
+typedef const __attribute__((address_space(1))) void *GlobalPtr;
+typedef __attribute__((address_space(3))) void *LdsPtr;
+__device__ inline void pieces_to_lds(uint64_t from, void *to) { __builtin_amdgcn_global_load_lds((GlobalPtr)from, (LdsPtr)to, 16, 0, 0); }
+__device__ inline void words_to_lds(uint64_t from, void *to) { __builtin_amdgcn_global_load_lds((GlobalPtr)from, (LdsPtr)to, 4, 0, 0); }
+
+// a token's scales and offsets as an operand: the first words of a lane's sixteen bytes
+template <int kWords, class Words> __device__ inline u32x4 operand(Words v)
+{
+    u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) r[w] = v[w];
+    return r;
+}
+
 // Rows of one sequence and K/V head: row r is new token r / G, head G * kv_head + r % G.
 struct Rows {
     int64_t first, next, tokens, length, capacity;
@@ -214,12 +229,17 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                                                            int64_t ots, int64_t ohs, float scale, int32_t causal, int32_t max_q, uint32_t row_sets, int32_t splits, int32_t unit, float *scratch)
 {
     constexpr int kGroups = D / 32, kChannelTiles = D / 16, kQueries = kFew ? 16 / kGroups : 16, kRows = kQueries * kTiles;
-    constexpr int kPitch = D / 2 + 16;              // bytes of a token's values in LDS
-    __shared__ union {                              // the waves' values, and after the last key their results
-        __attribute__((aligned(16))) uint8_t values[4][64 * kPitch];
-        float joined[4][kQueries][D + 4];
+    typedef uint32_t Words __attribute__((ext_vector_type(kGroups)));       // a lane's codes, and a token's scales and offsets
+    struct Tile {                                   // as in the pages, but a value's 16-byte pieces lie at place piece ^ (token / 4)
+        u32x4 keys[64 * D / 32], values[64 * D / 32];
+        Words key_params[64], value_params[64];
+    };
+    __shared__ union {                              // the waves' tiles, and after the last key their results
+        Tile tiles[4][2];                           // with D = 128 half of a compute unit's 160 KiB to the byte
+        struct {
+            float joined[4][kQueries][D + 4], stats[2][4][kTiles][16];
+        } end;
     } lds;
-    __shared__ float stats[2][4][kTiles][16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
     // Heads first, then sequences, then sets of rows from the last one on (they attend to the most), then splits: neighbouring
     // work-groups go to different XCDs, and what neighbours have to do should be alike.
@@ -283,10 +303,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) most[t] = -INFINITY;
 
-    // ---- a tile's codes, scales and offsets are asked for one tile ahead, its page numbers two ----
-    typedef uint32_t Words __attribute__((ext_vector_type(kGroups)));       // a lane's codes, and a token's scales and offsets
-    Words kc[4], vc[4], kp[4], vp[4];
-    uint32_t bad = 0;                               // 16 keys in a page that is none
+    // ---- a tile goes from its pages to LDS one tile ahead, its page numbers are looked up two tiles ahead ----
+    uint32_t bad_ahead = 0;                         // 16 keys in a page that is none
     int32_t page_ahead = -1;                        // of 16 keys each: lane l has the tile's part l % 4
     uint32_t slot_ahead = 0;
     const uint32_t page_blocks = (uint32_t)c.page_size / 16;
@@ -297,49 +315,61 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         page_ahead = -1;
         if (at < (uint32_t)c.table_width) page_ahead = c.table[(int64_t)b * c.table_width + at];
     };
-    const auto fetch = [&]() __attribute__((always_inline)) {
+    const auto fetch = [&](Tile &to) __attribute__((always_inline)) {
         // a page behind the table or outside the pool: page 0 instead, and its keys do not count
         const bool none = page_ahead < 0 || page_ahead >= c.pages;
-        bad = (uint32_t)__ballot(none) & 15;
+        bad_ahead = (uint32_t)__ballot(none) & 15;
         const uint64_t page = (uint64_t)(none ? 0 : page_ahead) * c.kv_heads + rows.kv_head;
         const uint64_t base = (uint64_t)c.pool + page * (uint64_t)c.page_bytes();
         const uint64_t codes = base + slot_ahead * (D / 2), params = base + params_after + slot_ahead * (D / 8);
+        const auto of_lane = [&](uint64_t v, int i) __attribute__((always_inline)) {
+            return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i);
+        };
+        // 16 keys are D/2 pieces of 16 bytes of codes and D/2 words of scales and offsets: 64 lanes take 16 keys (D = 128) or 32
+        constexpr int kEach = 64 / (D / 2), kPieces = D / 32;                // parts of a load, pieces of a token
+        const int in = lane % (D / 2), token = in / kPieces, swapped = token * kPieces + (in % kPieces ^ token / 4 % kPieces);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const auto of_lane = [&](uint64_t v) __attribute__((always_inline)) {
-                return (const uint8_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 |
-                                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, i));
-            };
-            const uint8_t *k = of_lane(codes), *s = of_lane(params);
-            kc[i] = ((const Words *)k)[col * 4 + h];
-            kp[i] = ((const Words *)s)[col];
-            vc[i] = ((const Words *)(k + value_codes))[lane];
-            vp[i] = ((const Words *)(s + value_params))[col];
+        for (int i = 0; i < 4; i += kEach) {
+            uint64_t k = of_lane(codes, i), s = of_lane(params, i);
+            if constexpr (kEach == 2) {
+                const uint64_t k1 = of_lane(codes, i + 1), s1 = of_lane(params, i + 1);
+                k = lane < 32 ? k : k1;
+                s = lane < 32 ? s : s1;
+            }
+            pieces_to_lds(k + 16 * in, &to.keys[i * (D / 2)]);
+            pieces_to_lds(k + value_codes + 16 * swapped, &to.values[i * (D / 2)]);
+            words_to_lds(s + 4 * in, &to.key_params[16 * i]);
+            words_to_lds(s + value_params + 4 * in, &to.value_params[16 * i]);
         }
     };
     const ppmm::Unpacker<T> unpack;
     const ppmm::Unpacker<BF16> unpack_values;
-    uint8_t *shared = lds.values[wave];
-    int32_t k0 = (int32_t)begin + 64 * wave;        // lengths are below 2^31, and a tile ends behind them by 320 at the most
+    Tile *const tiles = lds.tiles[wave];
+    int32_t k0 = (int32_t)begin + 64 * wave;        // lengths are below 2^31
     if (k0 < end) {
         look_ahead(k0);
-        fetch();
+        fetch(tiles[0]);
         if (k0 < end - 256) look_ahead(k0 + 256);
     }
-    for (; k0 < end; k0 = k0 < end - 256 ? k0 + 256 : end) {
-        const uint32_t wrong = bad;
+    for (int turn = 0; k0 < end; k0 = k0 < end - 256 ? k0 + 256 : end, turn ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the tile is in LDS; it is this wave's alone
+        const Tile &now = tiles[turn];
+        const uint32_t wrong = bad_ahead;
+        if (k0 < end - 256) {
+            fetch(tiles[turn ^ 1]);
+            if (k0 < end - 512) look_ahead(k0 + 512);
+        }
         const bool whole = k0 <= clear - 64 && !wrong;
         // ---- scores ----
         f32x4 p[kTiles][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            u32x4 params = {0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < kGroups; ++w) params[w] = kp[i][w];
+            const u32x4 params = operand<kGroups>(now.key_params[16 * i + col]);
+            const Words codes = ((const Words *)now.keys)[(16 * i + col) * 4 + h];
             const f32x4 zero = {0, 0, 0, 0}, s = BF16::mma(params, one_s, zero);
             u32x4 keys[kGroups];
 #pragma unroll
-            for (int j = 0; j < kGroups; ++j) keys[j] = unpack.template get<kKeyBit>(kc[i][j]);
+            for (int j = 0; j < kGroups; ++j) keys[j] = unpack.template get<kKeyBit>(codes[j]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 f32x4 score = BF16::mma(params, qsum[t], zero);
@@ -371,20 +401,50 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                 p[t][i] = score * scale;
             }
         }
-        if (!whole) {
+        if (!whole)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t key = 16 * i + 4 * h;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (key + e >= limit[t] - k0 || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
-                // values that do not count: whatever lies there, its scale and offset are zero
-                const bool none = 16 * i + col >= held - k0 || (wrong >> i & 1);
+                        if (16 * i + 4 * h + e >= limit[t] - k0 || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
+        // ---- probabilities: the largest score counts from where it was unless it grew by more than 2^8 ----
 #pragma unroll
-                for (int w = 0; w < kGroups; ++w) vp[i][w] = none ? 0 : vp[i][w];
+        for (int t = 0; t < kTiles; ++t) {
+            float top = fmaxf(fmaxf(p[t][0][0], p[t][0][1]), fmaxf(p[t][0][2], p[t][0][3]));
+#pragma unroll
+            for (int i = 1; i < 4; ++i) top = fmaxf(top, fmaxf(fmaxf(p[t][i][0], p[t][i][1]), fmaxf(p[t][i][2], p[t][i][3])));
+            top = most_of_quarters(top);
+            const bool grew = top > most[t] + 8.0f || most[t] == -INFINITY;
+            if (__ballot(grew && top != -INFINITY)) {
+                const float now = grew ? fmaxf(top, most[t]) : most[t];
+                const float keep = most[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most[t] - now);
+                most[t] = now;
+                sum[t] *= keep;
+#pragma unroll
+                for (int n = 0; n < kSums; ++n) z[t][n] *= keep;
+#pragma unroll
+                for (int n = 0; n < kChannelTiles; ++n) o[t][n] *= keep;
             }
+            const float from = most[t] == -INFINITY ? 0.0f : most[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[t][i][e] = __builtin_amdgcn_exp2f(p[t][i][e] - from);
+                    sum[t] += p[t][i][e];
+                }
+        }
+        // ---- values ----
+        Words vp[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vp[i] = now.value_params[16 * i + col];
+            // values that do not count: whatever lies there, scale and offset are zero
+            if (!whole)
+#pragma unroll
+                for (int w = 0; w < kGroups; ++w) vp[i][w] = 16 * i + col >= held - k0 || (wrong >> i & 1) ? 0 : vp[i][w];
         }
         // Groups of values that read as NaN: their offset would spoil other groups and rows that do not attend to them (0 * NaN).  It is
         // taken out, and the sums of the rows that do attend to them become NaN.
@@ -428,52 +488,18 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                 }
             }
         }
-        // ---- probabilities: the largest score counts from where it was unless it grew by more than 2^8 ----
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            float top = fmaxf(fmaxf(p[t][0][0], p[t][0][1]), fmaxf(p[t][0][2], p[t][0][3]));
-#pragma unroll
-            for (int i = 1; i < 4; ++i) top = fmaxf(top, fmaxf(fmaxf(p[t][i][0], p[t][i][1]), fmaxf(p[t][i][2], p[t][i][3])));
-            top = most_of_quarters(top);
-            const bool grew = top > most[t] + 8.0f || most[t] == -INFINITY;
-            if (__ballot(grew && top != -INFINITY)) {
-                const float now = grew ? fmaxf(top, most[t]) : most[t];
-                const float keep = most[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most[t] - now);
-                most[t] = now;
-                sum[t] *= keep;
-#pragma unroll
-                for (int n = 0; n < kSums; ++n) z[t][n] *= keep;
-#pragma unroll
-                for (int n = 0; n < kChannelTiles; ++n) o[t][n] *= keep;
-            }
-            const float from = most[t] == -INFINITY ? 0.0f : most[t];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[t][i][e] = __builtin_amdgcn_exp2f(p[t][i][e] - from);
-                    sum[t] += p[t][i][e];
-                }
-        }
-        // ---- values ----
         f32x4 s[4], off[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            u32x4 params = {0, 0, 0, 0};
-#pragma unroll
-            for (int w = 0; w < kGroups; ++w) params[w] = vp[i][w];
+            const u32x4 params = operand<kGroups>(vp[i]);
             s[i] = BF16::mma(params, one_s, f32x4{0, 0, 0, 0});
             off[i] = BF16::mma(params, one_b, f32x4{0, 0, 0, 0});
-            *(Words *)(shared + (16 * i + lane / 4) * kPitch + lane % 4 * 4 * kGroups) = vc[i];
         }
-        if (k0 < end - 256) {
-            fetch();
-            if (k0 < end - 512) look_ahead(k0 + 512);
-        }
-        const uint8_t *from = shared + (16 * (col / 4) + 4 * h + col % 4) * kPitch;
+        const int token = 16 * (col / 4) + 4 * h + col % 4;      // whose values this lane hands in
+        const uint8_t *from = (const uint8_t *)now.values + token * (D / 2);
         const auto add_values = [&](int n, const u32x4 (&big)[kTiles][2], const u32x4 (&small)[kTiles][2]) __attribute__((always_inline)) {
             typedef int v2i __attribute__((ext_vector_type(2)));
-            const v2i w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i *)(from + 8 * n));
+            const v2i w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i *)(from + 16 * (n / 2 ^ h % (D / 32)) + 8 * (n % 2)));
             const u32x4 v0 = unpack_values.get<0>((uint32_t)w[0]), v1 = unpack_values.get<0>((uint32_t)w[1]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
@@ -528,14 +554,15 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     }
 
     // ---- the four waves' parts together ----
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         sum[t] = across_quarters(sum[t]);
 #pragma unroll
         for (int n = 0; n < kSums; ++n) z[t][n] = across_quarters(z[t][n]);
         if (h == 0) {
-            stats[0][wave][t][col] = most[t];
-            stats[1][wave][t][col] = sum[t];
+            lds.end.stats[0][wave][t][col] = most[t];
+            lds.end.stats[1][wave][t][col] = sum[t];
         }
     }
     __syncthreads();
@@ -543,25 +570,25 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     for (int t = 0; t < kTiles; ++t) {
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[0][w][t][col]);
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.end.stats[0][w][t][col]);
         const float keep = most[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(most[t] - top);
         if (t) __syncthreads();
 #pragma unroll
         for (int n = 0; n < kChannelTiles; ++n)
             if (!kFew || mine == n / 2)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) lds.joined[wave][query][16 * n + 4 * h + e] = (o[t][n][e] + z[t][kFew ? 0 : n / 2]) * keep;
+                for (int e = 0; e < 4; ++e) lds.end.joined[wave][query][16 * n + 4 * h + e] = (o[t][n][e] + z[t][kFew ? 0 : n / 2]) * keep;
         __syncthreads();
         for (int i = threadIdx.x; i < kQueries * D; i += 256) {
             const int k = i / D, ch = i % D;
             float m = -INFINITY, l = 0.0f, v = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[0][w][t][k]);
+            for (int w = 0; w < 4; ++w) m = fmaxf(m, lds.end.stats[0][w][t][k]);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float mw = stats[0][w][t][k];
-                l += mw == -INFINITY ? 0.0f : stats[1][w][t][k] * __builtin_amdgcn_exp2f(mw - m);
-                v += lds.joined[w][k][ch];
+                const float mw = lds.end.stats[0][w][t][k];
+                l += mw == -INFINITY ? 0.0f : lds.end.stats[1][w][t][k] * __builtin_amdgcn_exp2f(mw - m);
+                v += lds.end.joined[w][k][ch];
             }
             const uint32_t r = row0 + t * kQueries + k;
             const int64_t n = rows.token(r);
@@ -585,7 +612,7 @@ __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int3
     const int lane = threadIdx.x % 64;
     const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, n = row / heads;
     if (n >= tokens) return;
-    const int32_t b = c.sequence_of(n);
+    const int32_t b = c.sequence_of_wave(n);
     if (b < 0 || n - c.starts[b] >= max_q) return;
     const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits, unit);
     const int used = held > part ? (int)((held + part - 1) / part) : 1;

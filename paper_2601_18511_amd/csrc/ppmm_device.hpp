@@ -85,6 +85,21 @@ struct Cache {
         return starts[lo] <= n && n < starts[lo + 1] ? lo : -1;
     }
 
+    // The same for a wave that looks for one row together: 64 places at a time.
+    __device__ int32_t sequence_of_wave(int64_t n) const
+    {
+        const int lane = threadIdx.x % 64;
+        int32_t lo = 0;
+        for (int32_t left = batch; left > 1;) {             // the sequence is among lo ... lo + left - 1
+            const int32_t stride = (left + 63) / 64, at = lane * stride;
+            const int below = __popcll(__ballot(at < left && starts[lo + (at < left ? at : 0)] <= n));
+            if (below == 0) return -1;
+            lo += (below - 1) * stride;
+            left = left - (below - 1) * stride < stride ? left - (below - 1) * stride : stride;
+        }
+        return starts[lo] <= n && n < starts[lo + 1] ? lo : -1;
+    }
+
     // start of the page of head h that holds token `position` of sequence b, or null
     __device__ uint8_t *page_of(int32_t b, int64_t position, int32_t h) const
     {
