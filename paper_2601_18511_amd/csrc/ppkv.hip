@@ -401,7 +401,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                 p[t][i] = score * scale;
             }
         }
-        if (!whole)
+        if (!whole) {
+            asm volatile("");                       // a branch, not 48 selects in every tile
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -409,6 +410,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (16 * i + 4 * h + e >= limit[t] - k0 || (wrong >> i & 1)) p[t][i][e] = -INFINITY;
+        }
         // ---- probabilities: the largest score counts from where it was unless it grew by more than 2^8 ----
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -441,8 +443,12 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             vp[i] = now.value_params[16 * i + col];
+        }
+        if (!whole) {
+            asm volatile("");
             // values that do not count: whatever lies there, scale and offset are zero
-            if (!whole)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int w = 0; w < kGroups; ++w) vp[i][w] = 16 * i + col >= held - k0 || (wrong >> i & 1) ? 0 : vp[i][w];
         }
@@ -604,19 +610,20 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     }
 }
 
-// Joins the splits of a row: one wave a row and head.
+// Joins the splits of a row, of which there are at most 64: a work-group a row and head, whose waves share the splits out.  Every lane
+// looks at one split's maximum and sum; four splits' results are under way at a time.
 template <class T, int D>
 __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int32_t heads, uint16_t *out, int64_t ots, int64_t ohs, int32_t max_q, int32_t splits,
                                                    int32_t unit, const float *scratch)
 {
-    const int lane = threadIdx.x % 64;
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, n = row / heads;
-    if (n >= tokens) return;
+    constexpr int E = D / 64;
+    __shared__ float part_sums[4][D];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t row = blockIdx.x, n = row / heads;
     const int32_t b = c.sequence_of_wave(n);
-    if (b < 0 || n - c.starts[b] >= max_q) return;
+    if (b < 0 || n - c.starts[b] >= max_q) return;              // the whole work-group
     const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits, unit);
     const int used = held > part ? (int)((held + part - 1) / part) : 1;
-    // a lane looks at one split's maximum and sum (there are at most 64), then all lanes take the weighted rows together
     const float *from = scratch + row * splits * (D + 2);
     const bool live = lane < used;
     const float mine = live ? from[lane * (D + 2) + D] : -INFINITY, mine_sum = live ? from[lane * (D + 2) + D + 1] : 0.0f;
@@ -624,17 +631,31 @@ __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int3
 #pragma unroll
     for (int step = 32; step; step /= 2) m = fmaxf(m, __shfl_xor(m, step));
     const float keep = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - m);
-    float l = keep * mine_sum, v[D / 64] = {};
+    float l = keep * mine_sum, v[E] = {};
 #pragma unroll
     for (int step = 32; step; step /= 2) l += __shfl_xor(l, step);
-    for (int s = 0; s < used; ++s) {
-        const float w = __shfl(keep, s);
+    for (int s0 = 4 * wave; s0 < used; s0 += 16) {
+        float x[4][E], w[4];
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[e] = fmaf(w, from[s * (D + 2) + lane * (D / 64) + e], v[e]);
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + i < used ? s0 + i : used - 1;
+            w[i] = s0 + i < used ? __shfl(keep, s) : 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = from[s * (D + 2) + lane * E + e];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = fmaf(w[i], x[i][e], v[e]);
     }
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e)
-        out[n * ots + row % heads * ohs + lane * (D / 64) + e] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : v[e] / l);
+    for (int e = 0; e < E; ++e) part_sums[wave][lane * E + e] = v[e];
+    __syncthreads();
+    const int ch = threadIdx.x;
+    if (ch < D) {
+        const float sum = part_sums[0][ch] + part_sums[1][ch] + part_sums[2][ch] + part_sums[3][ch];
+        out[n * ots + row % heads * ohs + ch] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : sum / l);
+    }
 }
 
 Cache device_cache(const ppkv_cache *c, const ppkv_batch *b)
@@ -723,7 +744,7 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
     const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len);
     if (d.splits > 1 && (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ppkv_attention_scratch_bytes(cache, batch, tokens, heads, max_q, max_len, device)))
         return PCMM_EINVAL;
-    const int64_t join_blocks = (tokens * heads + 3) / 4;
+    const int64_t join_blocks = tokens * heads;
     const int64_t blocks = d.row_sets * d.splits * cache->kv_heads;                               // of one sequence
     if (blocks > 0xffffff / batch->batch || join_blocks > 0xffffff) return PCMM_EUNSUPPORTED;     // no launch of 2^32 threads
     pcmm_hip_util::DevGuard dg(device);
