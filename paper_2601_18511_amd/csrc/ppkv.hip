@@ -50,30 +50,46 @@ __device__ inline uint32_t code_of(uint32_t word, int which, int i)       // cha
 }
 
 // ---- writing -------------------------------------------------------------------------------------------------------
-// A thread takes eight channels (16 bytes), four neighbouring threads a group.
+// The sequence of every lane's row.  A wave's rows follow one another: it looks for one after the other together.
+__device__ inline int32_t sequences(const Cache &c, int64_t n)
+{
+    const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane((int)n), last = (int64_t)__builtin_amdgcn_readlane((int)n, 63);      // below 2^31
+    int32_t mine = -1;
+    for (int64_t t = first; t <= last; ++t) {
+        const int32_t b = c.sequence_of_wave(t);
+        if (n == t) mine = b;
+    }
+    return mine;
+}
+
+// A thread takes eight channels (16 bytes), four neighbouring threads a group.  The grid is filled up to whole waves, and a lane
+// without a row looks for its sequence with the others.
+//
+// A code is rint((x - b) / s) - 16 of the 64-bit quotient.  In 32 bits the quotient is off by less than `unsure`, so its nearest
+// whole number is the right one unless it is that close to the middle of two; only then it is divided in 64 bits.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(Cache c, int64_t tokens, const uint16_t *k, int64_t kts, int64_t khs,
                                                           const uint16_t *v, int64_t vts, int64_t vhs)
 {
     const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int part = (int)(idx % (D / 8));
-    const int64_t row = idx / (D / 8);              // (token, K or V, head)
-    const int head = (int)(row % c.kv_heads);
-    const int which = (int)(row / c.kv_heads % 2);
-    const int64_t n = row / c.kv_heads / 2;
-    if (n >= tokens) return;                        // whole groups of threads leave together
-    const int32_t b = c.sequence_of(n);
-    if (b < 0) return;
+    const uint32_t row = (uint32_t)(idx / (D / 8)); // (token, K or V, head): below 2^32 threads
+    const int head = (int)(row % (uint32_t)c.kv_heads);
+    const int which = (int)(row / (uint32_t)c.kv_heads % 2);
+    const int64_t n = row / (uint32_t)c.kv_heads / 2;
+    u32x4 bits = {0, 0, 0, 0};                      // asked for before the place is looked up
+    if (n < tokens) __builtin_memcpy(&bits, (which ? v + n * vts + head * vhs : k + n * kts + head * khs) + part * 8, 16);
+    const int32_t b = sequences(c, n);
+    if (n >= tokens || b < 0) return;               // whole groups of threads leave together
     const int64_t position = (int64_t)c.lens[b] - (c.starts[b + 1] - n);
     uint8_t *page = c.page_of(b, position, head);
     if (!page) return;
-    const uint16_t *src = (which ? v + n * vts + head * vhs : k + n * kts + head * khs) + part * 8;
     float x[8];
     float low = INFINITY, high = -INFINITY;
     bool finite = true;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        x[i] = ppmm::to_f32<T>(src[i]);
+        x[i] = ppmm::to_f32<T>((uint16_t)(bits[i / 2] >> (16 * (i % 2))));
         finite = finite && isfinite(x[i]);
         low = fminf(low, x[i]);
         high = fmaxf(high, x[i]);
@@ -89,12 +105,17 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Cache c, int64_t token
     if (!(s >= 0x1p-126f)) { s = 0.0f; s_bits = 0; }
     uint16_t b_bits = ppmm::from_f32<BF16>((float)((double)low - 16.0 * (double)s));
     if (!finite || !isfinite(s) || !isfinite(ppmm::to_f32<BF16>(b_bits))) { s = 0.0f; s_bits = 0; b_bits = 0x7fc0; }
-    const double off = (double)ppmm::to_f32<BF16>(b_bits);
     uint32_t word = 0;
+    if (s > 0.0f) {
+        // x - b is off by 2^-24 (|x| + |b|), 1 / s and the product by 2^-23 of the quotient, which is below 64: within 2^-21 (|b| / s + 64)
+        const float off = ppmm::to_f32<BF16>(b_bits), each = 1.0f / s, unsure = 0x1p-20f * (fabsf(off) * each + 64.0f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const double steps = s > 0.0f ? rint(((double)x[i] - off) / (double)s) - 16.0 : 0.0;
-        word |= (uint32_t)(int)fmin(fmax(steps, 0.0), 15.0) << (4 * i);
+        for (int i = 0; i < 8; ++i) {
+            const float quotient = (x[i] - off) * each;
+            float steps = rintf(quotient);
+            if (!(fabsf(quotient - steps) < 0.5f - unsure)) steps = (float)rint(((double)x[i] - (double)off) / (double)s);
+            word |= (uint32_t)(int)fminf(fmaxf(steps - 16.0f, 0.0f), 15.0f) << (4 * i);
+        }
     }
     const int slot = (int)(position % c.page_size);
     const int j = part / 4, h = part % 4;
@@ -121,13 +142,12 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
 {
     const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int part = (int)(idx % (D / 8));
-    const int64_t row = idx / (D / 8);
-    const int head = (int)(row % c.kv_heads);
-    const int which = (int)(row / c.kv_heads % 2);
-    const int64_t n = row / c.kv_heads / 2;
-    if (n >= tokens || !(which ? v : k)) return;
-    const int32_t b = c.sequence_of(n);
-    if (b < 0) return;
+    const uint32_t row = (uint32_t)(idx / (D / 8));
+    const int head = (int)(row % (uint32_t)c.kv_heads);
+    const int which = (int)(row / (uint32_t)c.kv_heads % 2);
+    const int64_t n = row / (uint32_t)c.kv_heads / 2;
+    const int32_t b = sequences(c, n);
+    if (n >= tokens || b < 0 || !(which ? v : k)) return;
     const int64_t position = (int64_t)c.lens[b] - (c.starts[b + 1] - n);
     const uint8_t *page = c.page_of(b, position, head);
     uint16_t *dst = (which ? v + n * vts + head * vhs : k + n * kts + head * khs) + part * 8;
@@ -141,9 +161,11 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
         s = ppmm::to_f32<BF16>(params[j]);
         off = ppmm::to_f32<BF16>(params[D / 32 + j]);
     }
+    u32x4 bits = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        dst[i] = as_result<T>(fmaf(s, 16.0f + (float)code_of(word, which, i), off), fixed);
+        bits[i / 2] |= (uint32_t)as_result<T>(fmaf(s, 16.0f + (float)code_of(word, which, i), off), fixed) << (16 * (i % 2));
+    __builtin_memcpy(dst, &bits, 16);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------
@@ -767,7 +789,7 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
             else launch(attention_kernel<T, 128, 1, false>, join_kernel<T, 128>);
         } else {
             if (d.few) launch(attention_kernel<T, 64, 1, true>, join_kernel<T, 64>);
-            else launch(attention_kernel<T, 64, 2, false>, join_kernel<T, 64>);
+            else launch(attention_kernel<T, 64, 1, false>, join_kernel<T, 64>);
         }
     };
     if (type == PPMM_BF16) by_shape(BF16());

@@ -108,8 +108,8 @@ inline Division divide(const ppkv_cache &c, const ppkv_batch &b, int32_t heads, 
     Division d;
     const int most = c.head_dim == 128 ? 2 : 1;     // tiles of few queries that a work-group takes
     d.few = rows <= most * per_tile;
-    d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : most == 2 ? 1 : 2;
-    const int64_t set = d.tiles * (d.few ? per_tile : 16);
+    d.tiles = d.few ? (int)((rows + per_tile - 1) / per_tile) : 1;
+    const int64_t set = d.few ? d.tiles * per_tile : 16;
     d.row_sets = rows > 0 ? (rows + set - 1) / set : 0;
     // Enough work-groups for the chip, none with less than a round of its four waves (256 keys).  While rows are few, also no split with
     // more than four rounds, and none with fewer unless the chip needs them: lengths differ, and starting and joining cost a

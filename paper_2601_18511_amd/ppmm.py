@@ -4,7 +4,6 @@ attention over it.  Same names as the C ABI, argument marshalling only; there is
 from __future__ import annotations
 
 import ctypes
-import math
 from typing import Optional
 
 import torch
@@ -190,19 +189,28 @@ def ppkv_cache_create(pages: int, page_size: int, kv_heads: int, head_dim: int, 
 
 
 def _batch(cache: PpkvCache, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor) -> _CBatch:
-    for name, t, dims in (("starts", starts, 1), ("lens", lens, 1), ("table", table, 2)):
-        if t.get_device() != cache.device or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous %d-D int32 tensor on the cache's device" % (name, dims))
-    if starts.shape[0] != lens.shape[0] + 1 or table.shape[0] != lens.shape[0]:
+    device = cache.device
+    shape, count = table.shape, lens.shape
+    if not (starts.dtype is lens.dtype is table.dtype is torch.int32 and starts.get_device() == lens.get_device() == table.get_device() == device
+            and starts.is_contiguous() and lens.is_contiguous() and table.is_contiguous() and len(shape) == 2 and len(count) == 1 and starts.dim() == 1):
+        raise ValueError("starts, lens (1-D) and table (2-D) must be contiguous int32 tensors on the cache's device")
+    if starts.shape[0] != count[0] + 1 or shape[0] != count[0]:
         raise ValueError("starts must have one entry more than lens, table one row for each of them")
-    return _CBatch(starts.data_ptr(), lens.data_ptr(), table.data_ptr(), lens.shape[0], table.shape[1])
+    return _CBatch(starts.data_ptr(), lens.data_ptr(), table.data_ptr(), count[0], shape[1])
 
 
-def _check_rows(cache: PpkvCache, name: str, t: torch.Tensor, heads: int, types) -> None:
-    if t.get_device() != cache.device or t.dtype not in types:
+_READ_TYPES = {**_TYPES, torch.int16: PPMM_INT16}
+
+
+def _packed(cache: PpkvCache, name: str, t: torch.Tensor, heads: int, types):
+    """(rows, type, (address, token stride, head stride)) of a [tokens][heads][head_dim] tensor on the cache's device with neighbouring channels"""
+    kind = types.get(t.dtype)
+    if kind is None or t.get_device() != cache.device:
         raise ValueError("%s must be on the cache's device, of type %s" % (name, " or ".join(str(x) for x in types)))
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, cache.head_dim) or t.stride(2) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != cache.head_dim or stride[2] != 1:
         raise ValueError("%s must be [tokens][%d][%d] with neighbouring channels" % (name, heads, cache.head_dim))
+    return shape[0], kind, (t.data_ptr(), stride[0], stride[1])
 
 
 def ppkv_append(cache: PpkvCache, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
@@ -210,12 +218,11 @@ def ppkv_append(cache: PpkvCache, k: torch.Tensor, v: torch.Tensor, starts: torc
     """Quantise the new tokens' keys and values ([tokens][kv_heads][head_dim]) into the cache. Row n belongs to the sequence b with
     starts[b] <= n < starts[b+1] and is its token lens[b] - (starts[b+1] - n), in page table[b][.. // page_size]. Asynchronous."""
     batch = _batch(cache, starts, lens, table)
-    for name, t in (("k", k), ("v", v)):
-        _check_rows(cache, name, t, cache.kv_heads, _TYPES)
-    if k.dtype != v.dtype or k.shape != v.shape:
+    rows, kind, k_at = _packed(cache, "k", k, cache.kv_heads, _TYPES)
+    v_rows, v_kind, v_at = _packed(cache, "v", v, cache.kv_heads, _TYPES)
+    if rows != v_rows or kind != v_kind:
         raise ValueError("k and v must have the same type and shape")
-    rc = load_library().ppkv_append(cache._c, batch, k.shape[0], _TYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-                                    v.stride(0), v.stride(1), cache.device, _handle(cache.device, stream))
+    rc = (_lib or load_library()).ppkv_append(cache._c, batch, rows, kind, *k_at, *v_at, cache.device, _handle(cache.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_append")
 
@@ -225,17 +232,14 @@ def ppkv_read(cache: PpkvCache, k: Optional[torch.Tensor], v: Optional[torch.Ten
     """The cached values of the same tokens into k and v ([tokens][kv_heads][head_dim], either may be None). int16 tensors get
     rint(value 2^frac_bits): an operand of pcmm_plan_create. Asynchronous."""
     batch = _batch(cache, starts, lens, table)
-    given = [t for t in (k, v) if t is not None]
-    if not given:
+    k_is = (None, None, (None, 0, 0)) if k is None else _packed(cache, "k", k, cache.kv_heads, _READ_TYPES)
+    v_is = (None, None, (None, 0, 0)) if v is None else _packed(cache, "v", v, cache.kv_heads, _READ_TYPES)
+    rows, kind = k_is[:2] if k is not None else v_is[:2]
+    if rows is None:
         raise ValueError("neither k nor v is wanted")
-    types = {**_TYPES, torch.int16: PPMM_INT16}
-    for t in given:
-        _check_rows(cache, "k" if t is k else "v", t, cache.kv_heads, types)
-        if t.dtype != given[0].dtype or t.shape != given[0].shape:
-            raise ValueError("k and v must have the same type and shape")
-    rows = [(t.data_ptr(), t.stride(0), t.stride(1)) if t is not None else (None, 0, 0) for t in (k, v)]
-    rc = load_library().ppkv_read(cache._c, batch, given[0].shape[0], types[given[0].dtype], int(frac_bits), *rows[0], *rows[1], cache.device,
-                                  _handle(cache.device, stream))
+    if k is not None and v is not None and k_is[:2] != v_is[:2]:
+        raise ValueError("k and v must have the same type and shape")
+    rc = (_lib or load_library()).ppkv_read(cache._c, batch, rows, kind, int(frac_bits), *k_is[2], *v_is[2], cache.device, _handle(cache.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_read")
 
@@ -251,14 +255,15 @@ def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts:
     """Enqueue attention of the new tokens' queries ([tokens][heads][head_dim]) over the cache; scale defaults to 1 / sqrt(head_dim).
     max_q: the largest number of new tokens of a sequence; max_len: the expected largest length. Asynchronous."""
     batch = _batch(cache, starts, lens, table)
-    if q.dim() != 3 or q.shape[1] == 0 or q.shape[1] % cache.kv_heads:
+    heads = q.shape[1] if q.dim() == 3 else 0
+    if heads == 0 or heads % cache.kv_heads:
         raise ValueError("q must be [tokens][heads][head_dim] with a multiple of the cache's heads")
-    for name, t in (("q", q), ("out", out)):
-        _check_rows(cache, name, t, q.shape[1], _TYPES)
-    if q.dtype != out.dtype or q.shape != out.shape:
+    tokens, kind, q_at = _packed(cache, "q", q, heads, _TYPES)
+    out_tokens, out_kind, out_at = _packed(cache, "out", out, heads, _TYPES)
+    if tokens != out_tokens or kind != out_kind:
         raise ValueError("q and out must have the same type and shape")
-    lib, device, tokens, heads = load_library(), cache.device, q.shape[0], q.shape[1]
-    size = lib.ppkv_attention_scratch_bytes(cache._c, batch, tokens, heads, int(max_q), int(max_len), device)
+    lib, device, max_q, max_len = _lib or load_library(), cache.device, int(max_q), int(max_len)
+    size = lib.ppkv_attention_scratch_bytes(cache._c, batch, tokens, heads, max_q, max_len, device)
     scratch = None
     if size:        # of the pool of the stream that uses it: whoever gets the memory next runs behind this call
         if stream is None:
@@ -266,8 +271,7 @@ def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts:
         else:
             with torch.cuda.stream(stream):
                 scratch = torch.empty(size, dtype=torch.uint8, device=cache.pool.device)
-    rc = lib.ppkv_attention(cache._c, batch, tokens, _TYPES[q.dtype], heads, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0),
-                            out.stride(1), 1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), int(bool(causal)), int(max_q),
-                            int(max_len), scratch.data_ptr() if size else None, size, device, _handle(device, stream))
+    rc = lib.ppkv_attention(cache._c, batch, tokens, kind, heads, *q_at, *out_at, cache.head_dim ** -0.5 if scale is None else float(scale),
+                            1 if causal else 0, max_q, max_len, scratch.data_ptr() if size else None, size, device, _handle(device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_attention")
