@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <new>
 
 #include "ppmm_device.hpp"
@@ -73,8 +74,8 @@ __global__ __launch_bounds__(256) void pack_params_kernel(const uint16_t *scales
 }
 
 // ---- a few tokens --------------------------------------------------------------------------------------------------
-// HBM-bound: the weights stream through once and every token rides along.  A work-group of kWaves waves takes kRows tiles of 16
-// rows (of both matrices, if gated) and kTok tiles of 16 tokens; its waves share out the blocks of K and add up through LDS.
+// HBM-bound: the weights stream through once and every token rides along.  A work-group of kWaves waves takes 16 rows (of both
+// matrices, if gated) and up to 16 tokens; its waves share out the blocks of K and add up through LDS.
 
 // Eight values of one token from k on, zero behind K.  Elements are aligned to two bytes; the loads take any such address.
 __device__ inline u32x4 load_x(const uint16_t *row, int64_t k, int64_t K)
@@ -154,27 +155,28 @@ __device__ inline void add_block(const ppmm::Unpacker<T> &unpack, f32x4 (&sum)[k
                 for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(o[e], base[t][g][e], sum[t][e]);
         }
     }
+    // The sums are finished here.  Sunk below a branch by the compiler they have read a matrix instruction's result too early: its
+    // hazard waits were missing on the way through the branch, and the hardware has none.
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) asm volatile("" : "+v"(sum[t]));
 }
 
-// Adds up what the waves left in part and stores 16 tokens from t0 on, 16 rows of kRows tiles; a thread finishes one result of each
-// tile it takes.
-template <class T, int kRows, int kWaves, bool kGated>
-__device__ inline void finish(const f32x4 (&part)[kWaves][kRows * (kGated ? 2 : 1)][64], int64_t tile0, int64_t t0, int64_t M, int64_t tokens, uint16_t *y,
-                              int64_t ldy)
+// Adds up what the waves left in part and stores 16 tokens of 16 rows: 256 threads finish a result each.
+template <class T, int kWaves, bool kGated>
+__device__ inline void finish(const f32x4 (&part)[kWaves][kGated ? 2 : 1][64], int64_t tile, int64_t M, int64_t tokens, uint16_t *y, int64_t ldy)
 {
     constexpr int kMats = kGated ? 2 : 1;
-    for (int i = threadIdx.x; i < kRows * 256; i += 64 * kWaves) {
-        const int r = i / 256, e = i % 4, l = i / 4 % 64;
-        float v[kMats];
+    if (threadIdx.x >= 256) return;
+    const int e = threadIdx.x % 4, l = threadIdx.x / 4;
+    float v[kMats];
 #pragma unroll
-        for (int w = 0; w < kMats; ++w) {
-            v[w] = 0.0f;
+    for (int w = 0; w < kMats; ++w) {
+        v[w] = 0.0f;
 #pragma unroll
-            for (int q = 0; q < kWaves; ++q) v[w] += part[q][w * kRows + r][l][e];
-        }
-        const int64_t m = (tile0 + r) * 16 + 4 * (l / 16) + e, n = t0 + l % 16;
-        if (m < M && n < tokens) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0], v[kMats - 1]) : v[0]);
+        for (int q = 0; q < kWaves; ++q) v[w] += part[q][w][l][e];
     }
+    const int64_t m = tile * 16 + 4 * (l / 16) + e, n = l % 16;
+    if (m < M && n < tokens) y[n * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0], v[kMats - 1]) : v[0]);
 }
 
 // Up to four tokens whose rows fit LDS together.  Columns without a token carry the last one's values and are not stored.  With x
@@ -216,66 +218,170 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
         group_sums<T, kGroups>(base[0], xs[0]);
 #pragma unroll
         for (int w = 0; w < kMats; ++w) add_block<T, 1, kGroups, kOffsets>(unpack, sum[w], codes[w], params[w], xs, base);
-        if (kb + kWaves < kblocks) fetch(kb + kWaves);
+        fetch(kb + kWaves < kblocks ? kb + kWaves : kb);
     }
 #pragma unroll
     for (int w = 0; w < kMats; ++w) part[wave][w][lane] = sum[w][0];
     __syncthreads();
-    finish<T, 1, kWaves, kGated>(part, tile, 0, M, tokens, y, ldy);
+    finish<T, kWaves, kGated>(part, tile, M, tokens, y, ldy);
 }
 
-// Any number of tokens; x comes from the caches as the matrix instruction wants it.
-template <class T, int kTok, int kRows, int kWaves, int kGroups, bool kGated, bool kOffsets>
+// Up to sixteen tokens of any length; x comes from the caches as the matrix instruction wants it.
+template <class T, int kWaves, int kGroups, bool kGated, bool kOffsets>
 __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens,
                                                                  const uint16_t *x, int64_t ldx, uint16_t *y, int64_t ldy)
 {
-    constexpr int kTiles = kRows * (kGated ? 2 : 1);
+    constexpr int kMats = kGated ? 2 : 1;
     using Par = Params<kGroups, kOffsets>;
-    __shared__ f32x4 part[kWaves][kTiles][64];
+    __shared__ f32x4 part[kWaves][kMats][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
-    const int64_t tiles = (M + 15) / 16, tile0 = (int64_t)blockIdx.x * kRows, t0 = (int64_t)blockIdx.y * 16 * kTok;
-    const ppmm::Unpacker<T> unpack;
-    f32x4 sum[kTiles][kTok] = {};
-    const u32x4 *codes_of[kTiles];
-    const uint16_t *params_of[kTiles];
+    const int64_t tile = blockIdx.x;
+    const uint16_t *row = x + col * ldx;
+    u32x4 codes[kMats];
+    Par params[kMats];
+    const auto fetch = [&](int kb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {              // a tile behind the last one is the last one once more
-        const Weights &w = i / kRows ? b : a;
-        const int64_t tile = tile0 + i % kRows < tiles ? tile0 + i % kRows : tiles - 1;
-        codes_of[i] = w.codes + tile * kblocks * 64 + lane;
-        params_of[i] = w.params + tile * kblocks * Par::kStride;
-    }
-    const uint16_t *row[kTok];
-#pragma unroll
-    for (int t = 0; t < kTok; ++t) row[t] = x + (t0 + 16 * t + col) * ldx;
-    for (int kb = wave; kb < kblocks; kb += kWaves) {
-        u32x4 codes[kTiles], xs[kTok][4];
-        Par params[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            codes[i] = codes_of[i][(int64_t)kb * 64];
-            params[i].load(params_of[i] + (int64_t)kb * Par::kStride, h);
+        for (int w = 0; w < kMats; ++w) {
+            const Weights &m = w ? b : a;
+            codes[w] = m.codes[(tile * kblocks + kb) * 64 + lane];
+            params[w].load(m.params + (tile * kblocks + kb) * Par::kStride, h);
         }
+    };
+    const ppmm::Unpacker<T> unpack;
+    f32x4 sum[kMats][1] = {};
+    if (wave < kblocks) fetch(wave);
+    for (int kb = wave; kb < kblocks; kb += kWaves) {
+        u32x4 xs[1][4];
 #pragma unroll
-        for (int t = 0; t < kTok; ++t)
+        for (int j = 0; j < 4; ++j) {
+            xs[0][j] = u32x4{0, 0, 0, 0};
+            if (col < tokens) xs[0][j] = load_x(row, (int64_t)kb * 128 + 32 * j + 8 * h, K);
+        }
+        f32x4 base[1][kGroups];
+        group_sums<T, kGroups>(base[0], xs[0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                xs[t][j] = u32x4{0, 0, 0, 0};
-                if (t0 + 16 * t + col < tokens) xs[t][j] = load_x(row[t], (int64_t)kb * 128 + 32 * j + 8 * h, K);
+        for (int w = 0; w < kMats; ++w) add_block<T, 1, kGroups, kOffsets>(unpack, sum[w], codes[w], params[w], xs, base);
+        fetch(kb + kWaves < kblocks ? kb + kWaves : kb);
+    }
+#pragma unroll
+    for (int w = 0; w < kMats; ++w) part[wave][w][lane] = sum[w][0];
+    __syncthreads();
+    finish<T, kWaves, kGated>(part, tile, M, tokens, y, ldy);
+}
+
+// ---- a batch of tokens ---------------------------------------------------------------------------------------------
+// Too many tokens to fetch x anew for every tile of rows, too few for large tiles.  Of a work-group's eight waves kRowWaves take 16
+// rows each (of both matrices, if gated) with the same 16 kTok tokens out of LDS; kWays such teams take one block of K in kWays each
+// and add up at the end.  Weights are asked for two steps ahead, x one.
+constexpr int kBatchWaves = 8;
+
+template <class T, int kTok, int kRowWaves, int kGroups, bool kGated, bool kOffsets>
+__global__ __launch_bounds__(64 * kBatchWaves) void batch_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t all_tokens,
+                                                                 const uint16_t *all_x, int64_t ldx, bool buffered, uint16_t *all_y, int64_t ldy)
+{
+    using Par = Params<kGroups, kOffsets>;
+    constexpr int kMats = kGated ? 2 : 1, kPieces = kTok * 16 * 16, kWays = kBatchWaves / kRowWaves, kLoads = kTok * 4 / kRowWaves;
+    __shared__ union {
+        u32x4 x[2][kWays][kPieces];                 // two steps in turn, the block of each team
+        f32x4 part[kWays - 1][kRowWaves][kMats][kTok][64];
+    } lds;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
+    const int team = wave / kRowWaves, member = wave % kRowWaves;
+    const int64_t t0 = (int64_t)blockIdx.y * 16 * kTok;
+    const int tokens = all_tokens - t0 < 16 * kTok ? (int)(all_tokens - t0) : 16 * kTok;
+    const uint16_t *x = all_x + t0 * ldx;
+    const int64_t tiles = (M + 15) / 16, own = (int64_t)blockIdx.x * kRowWaves + member, tile = own < tiles ? own : tiles - 1;
+    const auto rows = __builtin_amdgcn_make_buffer_rsrc((void *)x, 0, buffered ? (int)(((tokens - 1) * ldx + K) * 2) : 0, 0x00027000);
+    const auto stage = [&](int step) __attribute__((always_inline)) {       // this team's block: a member brings 4 kLoads tokens
+        const int kb = kWays * step + team;
+        u32x4 *to = lds.x[step % 2][team] + member * kLoads * 64;
+        int l = lane;
+        asm volatile("" : "+v"(l));                 // the addresses are not kept from step to step
+        if (buffered && (kb + 1) * 128 <= K) {
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) {
+                const int token = (member * kLoads + n) * 4 + l / 16;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)(to + 64 * n), 16,
+                                                         token * (int)ldx * 2 + ((l % 16 ^ token % 16) * 8 + kb * 128) * 2, 0, 0, 0);
             }
+        } else {
+#pragma unroll 1
+            for (int n = 0; n < kLoads; ++n) {
+                const int token = (member * kLoads + n) * 4 + l / 16;
+                to[64 * n + l] = token < tokens ? load_x(x + token * ldx, (int64_t)kb * 128 + 8 * (l % 16 ^ token % 16), K) : u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    struct Raw {
+        u32x4 codes[kMats];
+        Par params[kMats];
+    };
+    const auto fetch = [&](Raw &r, int step) __attribute__((always_inline)) {
+        const int kb = kWays * step + team < kblocks ? kWays * step + team : kblocks - 1;      // behind the last block x is zero
+#pragma unroll
+        for (int w = 0; w < kMats; ++w) {
+            const Weights &m = w ? b : a;
+            r.codes[w] = (m.codes + (tile * kblocks + kb) * 64)[lane];
+            r.params[w].load(m.params + (tile * kblocks + kb) * Par::kStride, h);
+        }
+    };
+    const int steps = (kblocks + kWays - 1) / kWays;
+    const ppmm::Unpacker<T> unpack;
+    f32x4 sum[kMats][kTok] = {};
+    Raw raw[2];
+    const auto take = [&](Raw &r, int step) __attribute__((always_inline)) {
+        // loads are counted in their order: this step's x is here, the weights asked for behind it may be under way
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMats * (1 + Par::kLoads)) : "memory");
+        __syncthreads();                            // everyone's x is, and nobody reads the other step's any more
+        if (step + 1 < steps) stage(step + 1);
+        asm volatile("" ::: "memory");
+        const Raw now = r;
+        fetch(r, step + 2);
+        const u32x4 *from = lds.x[step % 2][team] + col * 16;
+        u32x4 xs[kTok][4];
         f32x4 base[kTok][kGroups];
 #pragma unroll
-        for (int t = 0; t < kTok; ++t) group_sums<T, kGroups>(base[t], xs[t]);
+        for (int t = 0; t < kTok; ++t) {
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) add_block<T, kTok, kGroups, kOffsets>(unpack, sum[i], codes[i], params[i], xs, base);
+            for (int j = 0; j < 4; ++j) xs[t][j] = from[16 * t * 16 + ((4 * j + h) ^ col)];
+            group_sums<T, kGroups>(base[t], xs[t]);
+        }
+#pragma unroll
+        for (int w = 0; w < kMats; ++w) add_block<T, kTok, kGroups, kOffsets>(unpack, sum[w], now.codes[w], now.params[w], xs, base);
+    };
+    stage(0);
+    asm volatile("" ::: "memory");
+    fetch(raw[0], 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    fetch(raw[1], 1);
+    for (int step = 0; step < steps; step += 2) {
+        take(raw[0], step);
+        if (step + 1 < steps) take(raw[1], step + 1);
     }
+    __syncthreads();
+    if (team)
+#pragma unroll
+        for (int w = 0; w < kMats; ++w)
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) lds.part[team - 1][member][w][t][lane] = sum[w][t];
+    __syncthreads();
+    if (team || own >= tiles) return;
 #pragma unroll
     for (int t = 0; t < kTok; ++t) {
-        if (t) __syncthreads();
+        const int n = 16 * t + col;
+        if (n >= tokens) continue;
+        f32x4 v[kMats];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) part[wave][i][lane] = sum[i][t];
-        __syncthreads();
-        finish<T, kRows, kWaves, kGated>(part, tile0, t0 + 16 * t, M, tokens, y, ldy);
+        for (int w = 0; w < kMats; ++w) {
+            v[w] = sum[w][t];
+#pragma unroll
+            for (int q = 0; q < kWays - 1; ++q) v[w] += lds.part[q][member][w][t][lane];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t m = own * 16 + 4 * h + e;
+            if (m < M) all_y[(t0 + n) * ldy + m] = ppmm::from_f32<T>(kGated ? silu_times(v[0][e], v[kMats - 1][e]) : v[0][e]);
+        }
     }
 }
 
@@ -419,14 +525,16 @@ struct Call {
     hipStream_t stream;
 };
 
-template <class T, int kTok, int kRows, int kGroups, bool kGated> void launch_few(const Call &c)
+// x in aligned pieces, and 32-bit offsets in a tile of 128 tokens
+bool buffered(const Call &c) { return ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0 && c.ldx < (1 << 22); }
+
+template <class T, int kGroups, bool kGated> void launch_few(const Call &c)
 {
     const ppmv_plan *p = c.p, *u = c.u;
-    const int64_t tiles = (p->M + 15) / 16;
-    const dim3 grid((unsigned)((tiles + kRows - 1) / kRows), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
-    auto kernel = p->has_offsets ? few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, true> : few_tokens_kernel<T, kTok, kRows, 8, kGroups, kGated, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, c.y, c.ldy);
+    auto kernel = p->has_offsets ? few_tokens_kernel<T, 8, kGroups, kGated, true> : few_tokens_kernel<T, 8, kGroups, kGated, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p->M + 15) / 16)), dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, c.y,
+                       c.ldy);
 }
 
 template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(const Call &c)
@@ -446,25 +554,55 @@ template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
     const uint32_t row_tiles = (uint32_t)((p->M + rows - 1) / rows), token_tiles = (uint32_t)((c.T + kTileTokens - 1) / kTileTokens);
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? many_tokens_kernel<T, kGroups, kGated, true> : many_tokens_kernel<T, kGroups, kGated, false>;
-    const bool buffered = ((uintptr_t)c.x & 15) == 0 && c.ldx % 8 == 0 && c.ldx < (1 << 22);      // aligned pieces, 32-bit offsets in a tile
     // check_product: fewer than 2^24 tiles of 16 x 64, so these count in 32 bits and launch fewer than 2^32 threads
     hipLaunchKernelGGL(kernel, dim3((row_tiles * token_tiles + 7) / 8 * 8), dim3(256), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, row_tiles,
-                       token_tiles, c.x, c.ldx, buffered, c.y, c.ldy);
+                       token_tiles, c.x, c.ldx, buffered(c), c.y, c.ldy);
+}
+
+template <class T, int kTok, int kRowWaves, int kGroups, bool kGated> void launch_batch(const Call &c)
+{
+    const ppmv_plan *p = c.p, *u = c.u;
+    // two matrices in groups of 32 with offsets: no registers for more than 32 tokens
+    if constexpr (kGated && kGroups == 4 && kTok > 2)
+        if (p->has_offsets) return launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
+    const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
+    auto kernel = p->has_offsets ? batch_kernel<T, kTok, kRowWaves, kGroups, kGated, true> : batch_kernel<T, kTok, kRowWaves, kGroups, kGated, false>;
+    const dim3 grid((unsigned)(((p->M + 15) / 16 + kRowWaves - 1) / kRowWaves), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * kBatchWaves), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, buffered(c), c.y,
+                       c.ldy);
+}
+
+template <class T, int kRowWaves, int kGroups, bool kGated> void launch_batches(const Call &c)
+{
+    if (c.T <= 16) launch_batch<T, 1, kRowWaves, kGroups, kGated>(c);
+    else if (c.T <= 32) launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
+    else if (c.T <= 48) launch_batch<T, 3, kRowWaves, kGroups, kGated>(c);
+    else launch_batch<T, 4, kRowWaves, kGroups, kGated>(c);
 }
 
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
 {
-    if (c.T > 64) return launch_many<T, kGroups, kGated>(c);
+    const int64_t tiles = (c.p->M + 15) / 16, mats = kGated ? 2 : 1;
+    // x rows in LDS: at most 32 KiB, which leaves every compute unit its waves
     if (c.T <= 4 && c.T * c.p->K <= 16384) {
         // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
         // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.  (Two matrices in groups of 32 do not fit the registers then.)
         if constexpr (!(kGated && kGroups == 4)) {
             if (c.p->M <= 8192 && c.p->K > 8192) return launch_stream<T, 16, kGroups, kGated>(c);
         }
-        launch_stream<T, 8, kGroups, kGated>(c);
-    } else if (c.T <= 16) launch_few<T, 1, 1, kGroups, kGated>(c);
-    else if (c.T <= 32) launch_few<T, 2, 2, kGroups, kGated>(c);
-    else launch_few<T, 4, 2, kGroups, kGated>(c);
+        return launch_stream<T, 8, kGroups, kGated>(c);
+    }
+    // 16 tokens: 4096 -> 4096 6.3 us and 7.3 with x shared by two waves, 4096 -> 14336 gated 21.9 and 15.5 by four
+    if (c.T <= 16 && tiles * mats <= 512) return launch_few<T, kGroups, kGated>(c);
+    // Otherwise the least of what was measured at K = 4096 (in tenths of a microsecond; all three grow alike with K), with work-groups
+    // counted in rounds of the chip: x shared by two waves or by four, or large tiles.
+    const int64_t chunks = c.T <= 64 ? 1 : (c.T + 63) / 64, large = (tiles * mats + 7) / 8 * ((c.T + 127) / 128);
+    const double two = (kGated ? 165 : 130) * std::max(1.0, (tiles + 1) / 2 * chunks / 256.0);
+    const double four = (kGated ? 260 : 195) * std::max(1.0, (tiles + 3) / 4 * chunks / 256.0);
+    const double many = c.T <= 64 ? 1e30 : std::max(570.0, 1.47 * large);
+    if (many < two && many < four) return launch_many<T, kGroups, kGated>(c);
+    if (two < four) return launch_batches<T, 2, kGroups, kGated>(c);
+    launch_batches<T, 4, kGroups, kGated>(c);
 }
 
 template <class T, bool kGated> void by_group(const Call &c)
