@@ -6,8 +6,6 @@
 #include <math.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "ppmm_device.hpp"
 #include "ppmm_host.hpp"
 #include "pcmm_hip_util.hpp"
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
 //
 // Few queries (kFew): a column is a pair of group and query, 16 / (D/32) queries a tile: the products of all groups with their
 // scales are one instruction each, and lanes do not work on empty columns.  Otherwise a column is a query, and the groups follow one
-// another; the scale of group j then comes out in every (D/32)th column and is taken from there.
+// another.
 //
 // The four waves of a work-group share out the tiles of its keys and join at the end; where there are few rows, several
 // work-groups share out the keys of a row and a second kernel joins them.
@@ -199,10 +197,9 @@ __device__ inline float most_of_quarters(float v)
 }
 template <int kCtrl> __device__ inline float dpp(float v)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
 }
 constexpr int kRor4 = 0x124, kRor8 = 0x128;         // rotations of 16 lanes
-__host__ __device__ constexpr int quad_of(int lane, int period) { return period == 4 ? lane * 0x55 : lane ? 0xDD : 0x88; }   // every lane of a quad takes this one; period 2: of its own pair
 
 __device__ inline uint32_t high_part(float v) { return __builtin_bit_cast(uint32_t, v) & 0xffff0000u; }
 __device__ inline float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
@@ -285,7 +282,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
     const int32_t end = rows.limit(last) < begin + part ? rows.limit(last) : (int32_t)(begin + part);      // behind the keys of any row
     const int32_t clear = rows.limit(row0);         // keys in front of this belong to every row
 
-    const int mine = kFew ? col / kQueries : col % kGroups;                  // the group whose scale this column brings out
+    const int mine = kFew ? col / kQueries : 0;     // the column's group
     const int query = kFew ? col % kQueries : col;
     // the column's queries as the second operand, and its sums in three parts, one a quarter of the lanes
     u32x4 qs[kTiles][kGroups], qsum[kTiles];
@@ -311,15 +308,19 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
             qsum[t][(kGroups + j) / 2] |= (kGroups + j) % 2 ? p : p >> 16;
         }
     }
-    // a one that brings out the column's scale, and one for its offset
-    u32x4 one_s = {0, 0, 0, 0}, one_b = {0, 0, 0, 0};
+    // ones that bring out a scale and an offset: of the column's group, or of every group in all columns
+    constexpr int kSums = kFew ? 1 : kGroups;
+    u32x4 one_s[kSums], one_b[kSums];
 #pragma unroll
-    for (int j = 0; j < kGroups; ++j)
-        if (h == 0 && mine == j) {
-            one_s[j / 2] = j % 2 ? 0x3f800000u : 0x3f80u;
-            one_b[(kGroups + j) / 2] = (kGroups + j) % 2 ? 0x3f800000u : 0x3f80u;
-        }
-    constexpr int kSums = kFew ? 1 : kGroups;       // sums of p b that a lane keeps
+    for (int n = 0; n < kSums; ++n) {
+        one_s[n] = one_b[n] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j)
+            if (h == 0 && (kFew ? mine == j : n == j)) {
+                one_s[n][j / 2] = j % 2 ? 0x3f800000u : 0x3f80u;
+                one_b[n][(kGroups + j) / 2] = (kGroups + j) % 2 ? 0x3f800000u : 0x3f80u;
+            }
+    }
     f32x4 o[kTiles][kChannelTiles] = {};
     float z[kTiles][kSums] = {}, most[kTiles], sum[kTiles] = {};
 #pragma unroll
@@ -388,7 +389,10 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         for (int i = 0; i < 4; ++i) {
             const u32x4 params = operand<kGroups>(now.key_params[16 * i + col]);
             const Words codes = ((const Words *)now.keys)[(16 * i + col) * 4 + h];
-            const f32x4 zero = {0, 0, 0, 0}, s = BF16::mma(params, one_s, zero);
+            const f32x4 zero = {0, 0, 0, 0};
+            f32x4 s[kSums];
+#pragma unroll
+            for (int n = 0; n < kSums; ++n) s[n] = BF16::mma(params, one_s[n], zero);
             u32x4 keys[kGroups];
 #pragma unroll
             for (int j = 0; j < kGroups; ++j) keys[j] = unpack.template get<kKeyBit>(codes[j]);
@@ -401,7 +405,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                     for (int j = 0; j < kGroups; ++j) acc = T::mma(keys[j], qs[t][j], acc);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float v = fmaf(s[e], acc[e], score[e]);
+                        float v = fmaf(s[0][e], acc[e], score[e]);
                         v += dpp<kRor8>(v);
                         if constexpr (kGroups == 4) v += dpp<kRor4>(v);
                         score[e] = v;
@@ -411,14 +415,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
 #pragma unroll
                     for (int j = 0; j < kGroups; ++j) acc[j] = T::mma(keys[j], qs[t][j], zero);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        score[e] = fmaf(dpp<quad_of(0, kGroups)>(s[e]), acc[0][e], score[e]);
-                        score[e] = fmaf(dpp<quad_of(1, kGroups)>(s[e]), acc[1][e], score[e]);
-                        if constexpr (kGroups == 4) {
-                            score[e] = fmaf(dpp<quad_of(2, 4)>(s[e]), acc[kGroups - 2][e], score[e]);
-                            score[e] = fmaf(dpp<quad_of(3, 4)>(s[e]), acc[kGroups - 1][e], score[e]);
-                        }
-                    }
+                    for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) score[e] = fmaf(s[j][e], acc[j][e], score[e]);
                 }
                 p[t][i] = score * scale;
             }
@@ -493,35 +492,16 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                     flags[w] = (lo ? 0x3f80u : 0) | (hi ? 0x3f800000u : 0);
                     vp[i][w] = v & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
                 }
-                const f32x4 flag = BF16::mma(flags, one_b, f32x4{0, 0, 0, 0});
-                const auto poison = [&](int n, const f32x4 &f) __attribute__((always_inline)) {
+#pragma unroll
+                for (int n = 0; n < kSums; ++n) {
+                    const f32x4 flag = BF16::mma(flags, one_b[n], f32x4{0, 0, 0, 0});
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (f[e] != 0.0f && 16 * i + 4 * h + e < limit[t] - k0) z[t][n] = NAN;
-                };
-                if constexpr (kFew) poison(0, flag);
-                else {
-                    const auto of = [&](auto index) __attribute__((always_inline)) {
-                        constexpr int ctrl = quad_of(decltype(index)::value, kGroups);
-                        poison(decltype(index)::value, f32x4{dpp<ctrl>(flag[0]), dpp<ctrl>(flag[1]), dpp<ctrl>(flag[2]), dpp<ctrl>(flag[3])});
-                    };
-                    of(std::integral_constant<int, 0>());
-                    of(std::integral_constant<int, 1>());
-                    if constexpr (kGroups == 4) {
-                        of(std::integral_constant<int, 2>());
-                        of(std::integral_constant<int, 3>());
-                    }
+                            if (flag[e] != 0.0f && 16 * i + 4 * h + e < limit[t] - k0) z[t][n] = NAN;
                 }
             }
-        }
-        f32x4 s[4], off[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4 params = operand<kGroups>(vp[i]);
-            s[i] = BF16::mma(params, one_s, f32x4{0, 0, 0, 0});
-            off[i] = BF16::mma(params, one_b, f32x4{0, 0, 0, 0});
         }
         const int token = 16 * (col / 4) + 4 * h + col % 4;      // whose values this lane hands in
         const uint8_t *from = (const uint8_t *)now.values + token * (D / 2);
@@ -550,34 +530,19 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                     z[t][n] = fmaf(p[t][2 * half + 1][e], bj[2 * half + 1][e], z[t][n]);
                 }
         };
-        u32x4 big[kTiles][2], small[kTiles][2];
-        if constexpr (kFew) {
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) weigh(t, 0, s, off, big[t], small[t]);
+        for (int n = 0; n < kSums; ++n) {           // one group, or in every column its own
+            f32x4 s[4], off[4];
 #pragma unroll
-            for (int n = 0; n < kChannelTiles; ++n) add_values(n, big, small);
-        } else {
-            const auto group = [&](auto index) __attribute__((always_inline)) {
-                constexpr int j = decltype(index)::value, ctrl = quad_of(j, kGroups);
-                f32x4 sj[4], bj[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sj[i][e] = dpp<ctrl>(s[i][e]);
-                        bj[i][e] = dpp<ctrl>(off[i][e]);
-                    }
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) weigh(t, j, sj, bj, big[t], small[t]);
-                add_values(2 * j, big, small);
-                add_values(2 * j + 1, big, small);
-            };
-            group(std::integral_constant<int, 0>());
-            group(std::integral_constant<int, 1>());
-            if constexpr (kGroups == 4) {
-                group(std::integral_constant<int, 2>());
-                group(std::integral_constant<int, 3>());
+            for (int i = 0; i < 4; ++i) {
+                s[i] = BF16::mma(operand<kGroups>(vp[i]), one_s[n], f32x4{0, 0, 0, 0});
+                off[i] = BF16::mma(operand<kGroups>(vp[i]), one_b[n], f32x4{0, 0, 0, 0});
             }
+            u32x4 big[kTiles][2], small[kTiles][2];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) weigh(t, n, s, off, big[t], small[t]);
+#pragma unroll
+            for (int k = 0; k < kChannelTiles / kSums; ++k) add_values(n * (kChannelTiles / kSums) + k, big, small);
         }
     }
 
