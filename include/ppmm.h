@@ -62,8 +62,9 @@ size_t ppmv_plan_workspace_bytes(const ppmv_plan *plan);
  *   y_dev    device, T rows of M elements, row stride ldy >= M; must not overlap x_dev
  *
  * A result does not depend on the other tokens' values, but its last bits may depend on how many there are.  An x that is
- * not finite makes every result of its token NaN or infinite.  PCMM_EINVAL for null pointers, negative T, strides that
- * are too small, y_dev == x_dev; PCMM_EUNSUPPORTED for larger T or more than 2^24 tiles of 16 x 64 results.
+ * not finite makes every result of its token NaN or infinite, and so may a sum of 31 |x| over a group that 32-bit floating
+ * point does not hold.  PCMM_EINVAL for null pointers, negative T, strides that
+ * are too small, y_dev == x_dev; PCMM_EUNSUPPORTED for larger T or more than 2^22 tiles of 16 x 64 results.
  */
 pcmm_status ppmv_run(const ppmv_plan *plan, int64_t T, const void *x_dev, int64_t ldx, void *y_dev, int64_t ldy, void *stream);
 
@@ -132,7 +133,8 @@ pcmm_status ppkv_append(const ppkv_cache *cache, const ppkv_batch *batch, int64_
 
 /*
  * The values of the same tokens: the inverse of ppkv_append.  k_dev or v_dev may be NULL: not wanted.  The strides must
- * keep the rows apart.  PPMM_INT16 writes rint(value 2^frac_bits), ties to even, held to [-32768, 32639] and 0 for NaN:
+ * keep the rows apart.  A value is rounded to 32 bits first.  PPMM_INT16 writes rint(value 2^frac_bits), ties to even, held to
+ * [-32768, 32639] and 0 for NaN:
  * the 16-bit plaintext operand of pcmm_plan_create.  With the strides of [kv_heads][tokens][head_dim] every head's keys
  * are such an operand.  0 <= frac_bits <= 30, and 0 for the other types.
  */
@@ -146,10 +148,11 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
  *     out[n][h] = sum_i softmax_i( scale <q[n][h], key_i> ) value_i ,    key and value of head h / (heads / kv_heads) ,
  *
  * over the tokens i of the row's sequence, i < lens[b], and, if causal, i not behind the row's own token.  A row that
- * attends to nothing is zero.  A token behind a causal row does not reach it, whatever it holds.
+ * attends to nothing is zero.  A token behind a causal row does not reach it, whatever it holds; of the tokens that a row
+ * attends to, a NaN key makes the whole row NaN, and values that read as NaN make those 32 channels of it NaN.
  *
  *   q_dev, out_dev   device, [tokens][heads][head_dim] with strides; the rows of out_dev must be apart; out_dev != q_dev
- *   heads            a multiple of kv_heads, heads / kv_heads <= 65536
+ *   heads            a multiple of kv_heads, heads / kv_heads <= 65536; max_q heads / kv_heads below 2^31 - 64
  *   max_q            no sequence has more new tokens; rows beyond are left as they were
  *   max_len          expected largest lens[b], for the division of the work only (0: table_width * page_size)
  *   scratch          device, ppkv_attention_scratch_bytes(same sizes) bytes, aligned to 16 bytes, for this call alone until

@@ -36,7 +36,7 @@ inline pcmm_status check_product(int64_t M, int64_t K, int64_t T, const void *x,
     if (!x || !y || x == y) return PCMM_EINVAL;
     if (ldx != 0 && ldx < K) return PCMM_EINVAL;
     if (T > kMaxRows || ldx > kMaxStride / T || ldy > kMaxStride / T) return PCMM_EUNSUPPORTED;
-    if ((up(M, 16) / 16) * (up(T, 64) / 64) > ((int64_t)1 << 24)) return PCMM_EUNSUPPORTED;
+    if ((up(M, 16) / 16) * (up(T, 64) / 64) > ((int64_t)1 << 22)) return PCMM_EUNSUPPORTED;      // no launch of 2^32 threads, whatever the kernel
     return PCMM_OK;
 }
 
@@ -68,15 +68,15 @@ inline pcmm_status check_cache(const ppkv_cache *c, const ppkv_batch *b, int64_t
     return PCMM_OK;
 }
 
-inline bool read_strides_ok(int64_t token_stride, int64_t head_stride)
+inline bool read_strides_ok(int64_t tokens, int64_t token_stride, int64_t head_stride)
 {
-    return token_stride >= 0 && head_stride >= 0 && token_stride <= kMaxStride / 0x7fffffff * 1024 && head_stride <= kMaxStride;
+    return token_stride >= 0 && head_stride >= 0 && head_stride <= kMaxStride && token_stride <= ((int64_t)1 << 59) / (tokens > 0 ? tokens : 1);
 }
 
 // no two of tokens x heads rows of D elements overlap
 inline bool rows_apart(int64_t tokens, int64_t heads, int64_t D, int64_t token_stride, int64_t head_stride)
 {
-    if (!read_strides_ok(token_stride, head_stride)) return false;
+    if (!read_strides_ok(tokens, token_stride, head_stride)) return false;
     const bool token_inner = heads == 1 || (tokens > 0 && head_stride >= (tokens - 1) * token_stride + D);
     const bool head_inner = tokens <= 1 || token_stride >= (heads - 1) * head_stride + D;
     return (head_inner && (heads == 1 || head_stride >= D)) || (token_inner && (tokens <= 1 || token_stride >= D));

@@ -287,10 +287,12 @@ __global__ __launch_bounds__(64 * kBatchWaves) void batch_kernel(Weights a, Weig
     } lds;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
     const int team = wave / kRowWaves, member = wave % kRowWaves;
-    const int64_t t0 = (int64_t)blockIdx.y * 16 * kTok;
+    const int64_t tiles = (M + 15) / 16;
+    const uint32_t sets = (uint32_t)((tiles + kRowWaves - 1) / kRowWaves);     // of rows; the next tokens come behind them all
+    const int64_t t0 = (int64_t)(blockIdx.x / sets) * 16 * kTok;
     const int tokens = all_tokens - t0 < 16 * kTok ? (int)(all_tokens - t0) : 16 * kTok;
     const uint16_t *x = all_x + t0 * ldx;
-    const int64_t tiles = (M + 15) / 16, own = (int64_t)blockIdx.x * kRowWaves + member, tile = own < tiles ? own : tiles - 1;
+    const int64_t own = (int64_t)(blockIdx.x % sets) * kRowWaves + member, tile = own < tiles ? own : tiles - 1;
     const auto rows = __builtin_amdgcn_make_buffer_rsrc((void *)x, 0, buffered ? (int)(((tokens - 1) * ldx + K) * 2) : 0, 0x00027000);
     const auto stage = [&](int step) __attribute__((always_inline)) {       // this team's block: a member brings 4 kLoads tokens
         const int kb = kWays * step + team;
@@ -554,7 +556,7 @@ template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
     const uint32_t row_tiles = (uint32_t)((p->M + rows - 1) / rows), token_tiles = (uint32_t)((c.T + kTileTokens - 1) / kTileTokens);
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? many_tokens_kernel<T, kGroups, kGated, true> : many_tokens_kernel<T, kGroups, kGated, false>;
-    // check_product: fewer than 2^24 tiles of 16 x 64, so these count in 32 bits and launch fewer than 2^32 threads
+    // check_product: at most 2^22 tiles of 16 x 64, so these count in 32 bits and launch fewer than 2^32 threads
     hipLaunchKernelGGL(kernel, dim3((row_tiles * token_tiles + 7) / 8 * 8), dim3(256), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, row_tiles,
                        token_tiles, c.x, c.ldx, buffered(c), c.y, c.ldy);
 }
@@ -567,7 +569,7 @@ template <class T, int kTok, int kRowWaves, int kGroups, bool kGated> void launc
         if (p->has_offsets) return launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? batch_kernel<T, kTok, kRowWaves, kGroups, kGated, true> : batch_kernel<T, kTok, kRowWaves, kGroups, kGated, false>;
-    const dim3 grid((unsigned)(((p->M + 15) / 16 + kRowWaves - 1) / kRowWaves), (unsigned)((c.T + 16 * kTok - 1) / (16 * kTok)));
+    const dim3 grid((unsigned)(((p->M + 15) / 16 + kRowWaves - 1) / kRowWaves * ((c.T + 16 * kTok - 1) / (16 * kTok))));
     hipLaunchKernelGGL(kernel, grid, dim3(64 * kBatchWaves), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, buffered(c), c.y,
                        c.ldy);
 }
@@ -583,8 +585,8 @@ template <class T, int kRowWaves, int kGroups, bool kGated> void launch_batches(
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
 {
     const int64_t tiles = (c.p->M + 15) / 16, mats = kGated ? 2 : 1;
-    // x rows in LDS: at most 32 KiB, which leaves every compute unit its waves
-    if (c.T <= 4 && c.T * c.p->K <= 16384) {
+    // x in LDS: at most 30 KiB beside at most 32 KiB of the waves' sums
+    if (c.T <= 4 && c.T * c.p->K <= 14336) {
         // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
         // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.  (Two matrices in groups of 32 do not fit the registers then.)
         if constexpr (!(kGated && kGroups == 4)) {

@@ -23,7 +23,9 @@ int main()
     CHECK(check_product(16, 64, kMaxRows + 1, a, 64, b, 16, &nothing) == PCMM_EUNSUPPORTED);
     CHECK(check_product(16, 64, 2, a, INT64_MAX, b, 16, &nothing) == PCMM_EUNSUPPORTED);
     CHECK(check_product(kMaxRows, 64, kMaxRows, a, 64, b, kMaxRows, &nothing) == PCMM_EUNSUPPORTED);
-    CHECK(check_product(kMaxRows, 64, 1024, a, 64, b, kMaxRows, &nothing) == PCMM_OK);
+    CHECK(check_product(kMaxRows, 64, 256, a, 64, b, kMaxRows, &nothing) == PCMM_OK);
+    CHECK(check_product(kMaxRows, 64, 257, a, 64, b, kMaxRows, &nothing) == PCMM_EUNSUPPORTED);
+    CHECK(check_product(16, 64, kMaxRows, a, 64, b, 16, &nothing) == PCMM_OK);
 
     CHECK(check_weights(kMaxRows, 4096, 32, PPMM_FP16, a, b, 0) == PCMM_OK);
     CHECK(check_weights(kMaxRows, 4097, 32, PPMM_FP16, a, b, 0) == PCMM_EUNSUPPORTED);
@@ -37,6 +39,8 @@ int main()
     CHECK(!rows_apart(3, 2, 64, 127, 64) && !rows_apart(3, 2, 64, 64, 191) && !rows_apart(3, 2, 64, 0, 64) && !rows_apart(3, 1, 64, 63, 64));
     CHECK(!rows_apart(3, 2, 64, -128, 64) && !rows_apart(0x7fffffff, 2, 64, INT64_MAX, 64) && !rows_apart(2, 1024, 64, 64, INT64_MAX));
     CHECK(rows_apart(0, 2, 64, 128, 64));
+    // the last token of every sequence of a [batch][tokens][heads][D] array
+    CHECK(rows_apart(64, 8, 128, (int64_t)1 << 30, 128) && read_strides_ok(64, (int64_t)1 << 40, 128));
     // brute force over small strides
     for (int tokens = 1; tokens <= 4; ++tokens)
         for (int heads = 1; heads <= 4; ++heads)
@@ -51,6 +55,20 @@ int main()
                         }
                     if (rows_apart(tokens, heads, D, ts, hs)) CHECK(apart);      // what is accepted does not overlap
                 }
+    // attention's division of the work: every row and key has a place, a join never sees more than 64 splits
+    for (int D = 64; D <= 128; D += 64)
+        for (int kv = 1; kv <= 8; kv += 7)
+            for (int G = 1; G <= 9; ++G)
+                for (int batch = 1; batch <= 4096; batch *= 8)
+                    for (int max_q = 1; max_q <= 5000; max_q = max_q * 3 + 1)
+                        for (int64_t max_len = 0; max_len <= 1 << 22; max_len = max_len * 5 + 77) {
+                            const ppkv_cache c{(void *)0x1000, 1000, 64, kv, D};
+                            const ppkv_batch bt{(const int32_t *)a, (const int32_t *)a, (const int32_t *)a, batch, 1 << 16};
+                            const Division d = divide(c, bt, kv * G, max_q, max_len);
+                            const int64_t per = d.few ? d.tiles * (16 / (D / 32)) : 16;
+                            CHECK(d.splits >= 1 && d.splits <= 64 && d.unit % 256 == 0 && d.tiles >= 1 && d.tiles <= 2);
+                            CHECK(d.row_sets * per >= (int64_t)max_q * G && (d.row_sets - 1) * per < (int64_t)max_q * G);
+                        }
     std::printf("all checks held\n");
     return 0;
 }

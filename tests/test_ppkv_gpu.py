@@ -375,6 +375,46 @@ def test_streams_and_graphs(gpu_device, seqs):
         assert torch.equal(eager, want[1 - i])
 
 
+def test_the_last_tokens_of_a_padded_batch(gpu_device):
+    """Keys, values and queries as views of the last token of [batch][tokens][heads][channels] arrays: far apart rows."""
+    import torch
+
+    import paper_2601_18511_amd as pkg
+
+    b = Batch([(1, n) for n in (5, 40, 17)], 8, 2, 128, 16, "bfloat16", gpu_device, seed=13).fill()
+    want = _attend(b)
+    b.check_attention(want)
+    big = [torch.zeros((3, 1000, h, 128), dtype=torch.bfloat16, device=gpu_device) for h in (2, 2, 8, 8)]
+    for dst, src in zip(big, (torch.stack([x[-1] for x in b.k]), torch.stack([x[-1] for x in b.v]), b.q)):
+        dst[:, -1].copy_(src)
+    pkg.ppkv_append(b.cache, big[0][:, -1], big[1][:, -1], *b.where())
+    pkg.ppkv_attention(b.cache, big[2][:, -1], big[3][:, -1], *b.where(), max_q=1)
+    assert torch.equal(big[3][:, -1], want) and (big[3][:, :-1] == 0).all()
+
+
+def test_many_sequences_and_shared_pages(gpu_device):
+    """More sequences than a wave has lanes, all over the same public prefix: its pages stand in every row of the table."""
+    import torch
+
+    import paper_2601_18511_amd as pkg
+
+    n, B, page = 48, 300, 16
+    b = Batch([(1, n)], 4, 2, 64, page, "float16", gpu_device, seed=14).fill()
+    q = torch.randn((B, 4, 64), dtype=torch.float32).half()
+    starts = torch.arange(B + 1, dtype=torch.int32, device=gpu_device)
+    lens = torch.full((B,), n, dtype=torch.int32, device=gpu_device)
+    table = b.dtable.expand(B, -1).contiguous()
+    out = torch.empty_like(q, device=gpu_device)
+    pkg.ppkv_attention(b.cache, q.to(gpu_device), out, starts, lens, table, max_q=1)
+    for i in (0, 1, 63, 64, 65, 255, 299):
+        b.q = q[i:i + 1]
+        b.check_attention(out[i:i + 1])
+    k = torch.zeros((B, 2, 64), dtype=torch.float16, device=gpu_device)
+    pkg.ppkv_read(b.cache, k, None, starts, lens, table)
+    want = torch.from_numpy(oracle.held(b.k[0][-1:].double().numpy())).float().half()
+    assert torch.equal(k.cpu(), want.expand(B, 2, 64))
+
+
 def test_refusals(gpu_device):
     import torch
 

@@ -100,6 +100,26 @@ def test_gated_product_matches_the_oracle(gpu_device, M, K, T, group, dtype):
         _near(h, want, bound, dtype)
 
 
+@pytest.mark.parametrize("M,K,T,gated", [(64, 14336, 1, True), (40, 14337, 1, True), (64, 16384, 1, True), (16, 3584, 4, True), (16, 64, 70000, False),
+                                         (16, 40, 5000, True), (5000, 64, 60, False), (9000, 128, 16, True)])
+def test_sizes_at_the_limits_of_each_kernel(gpu_device, M, K, T, gated):
+    """The largest x that lies in LDS and the first that does not, very many tokens of few rows, many rows of a short contraction."""
+    import torch
+
+    import paper_2601_18511_amd as pkg
+
+    codes, scales, off, x = _case(M, K, T, 32, "bfloat16", True, M + K + T, gpu_device)
+    plan = _plan(codes, scales, off, K, 32, gpu_device)
+    y = torch.full((T, M), float("nan"), dtype=x.dtype, device=gpu_device)
+    g, b = _want(codes, scales, off, x, 32)
+    if gated:
+        pkg.ppmv_gated_run(plan, plan, x.to(gpu_device), y)
+        _near(y, oracle.silu(g) * g, 2.2 * b * (np.abs(g) + b + 1) + np.abs(g * g) * (np.abs(g) + 8) * 2.0 ** -22, "bfloat16")
+    else:
+        pkg.ppmv_run(plan, x.to(gpu_device), y)
+        _near(y, g, b, "bfloat16")
+
+
 def test_one_plan_as_gate_and_up(gpu_device):
     import torch
 
