@@ -306,7 +306,21 @@ __global__ __launch_bounds__(64 * kBatchWaves) void batch_kernel(Weights a, Weig
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)(to + 64 * n), 16,
                                                          token * (int)ldx * 2 + ((l % 16 ^ token % 16) * 8 + kb * 128) * 2, 0, 0, 0);
             }
-        } else {
+        } else if ((kb + 1) * 128 <= K) {           // rows that are not aligned: through registers
+            constexpr int kHold = kLoads > 4 ? kLoads / 2 : kLoads;      // 1, 2, 3, 4, 6 or 8 loads in all
+#pragma unroll
+            for (int n0 = 0; n0 < kLoads; n0 += kHold) {
+                u32x4 v[kHold];
+#pragma unroll
+                for (int n = 0; n < kHold; ++n) {
+                    const int token = (member * kLoads + n0 + n) * 4 + l / 16;
+                    v[n] = u32x4{0, 0, 0, 0};
+                    if (token < tokens) __builtin_memcpy(&v[n], x + token * ldx + (int64_t)kb * 128 + 8 * (l % 16 ^ token % 16), 16);
+                }
+#pragma unroll
+                for (int n = 0; n < kHold; ++n) to[64 * (n0 + n) + l] = v[n];
+            }
+        } else {                                    // the last block, part of it behind K
 #pragma unroll 1
             for (int n = 0; n < kLoads; ++n) {
                 const int token = (member * kLoads + n) * 4 + l / 16;
@@ -433,7 +447,7 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
             for (int n = 0; n < 8; ++n)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)(to + 64 * n), 16,
                                                          (wave * 32 + 4 * n + l / 16) * (int)ldx * 2 + ((l % 16 ^ (4 * n + l / 16) % 16) * 8 + kb * 128) * 2, 0, 0, 0);
-        } else {
+        } else {                                    // rows that are not aligned, or the last block and part of it behind K
 #pragma unroll 1
             for (int n = 0; n < 8; ++n) {
                 const int token = wave * 32 + 4 * n + l / 16;
