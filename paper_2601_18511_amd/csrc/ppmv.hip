@@ -447,7 +447,21 @@ __global__ __launch_bounds__(256, 2) void many_tokens_kernel(Weights a, Weights 
             for (int n = 0; n < 8; ++n)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)(to + 64 * n), 16,
                                                          (wave * 32 + 4 * n + l / 16) * (int)ldx * 2 + ((l % 16 ^ (4 * n + l / 16) % 16) * 8 + kb * 128) * 2, 0, 0, 0);
-        } else {                                    // rows that are not aligned, or the last block and part of it behind K
+        } else if ((kb + 1) * 128 <= K) {           // rows that are not aligned: through registers, four at a time (1000 tokens 4001 ->
+                                                    // 4099: 121 us, one at a time 160; aligned rows of that size take 64)
+#pragma unroll
+            for (int n0 = 0; n0 < 8; n0 += 4) {
+                u32x4 v[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int token = wave * 32 + 4 * (n0 + n) + l / 16;
+                    v[n] = u32x4{0, 0, 0, 0};
+                    if (token < held) __builtin_memcpy(&v[n], from + (t0 + token) * ldx + (int64_t)kb * 128 + 8 * (l % 16 ^ token % 16), 16);
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n) to[64 * (n0 + n) + l] = v[n];
+            }
+        } else {                                    // the last block, part of it behind K
 #pragma unroll 1
             for (int n = 0; n < 8; ++n) {
                 const int token = wave * 32 + 4 * n + l / 16;
