@@ -54,7 +54,7 @@ __device__ inline int32_t sequences(const Cache &c, int64_t n)
     const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane((int)n), last = (int64_t)__builtin_amdgcn_readlane((int)n, 63);      // below 2^31
     int32_t mine = -1;
     for (int64_t t = first; t <= last; ++t) {
-        const int32_t b = c.sequence_of_wave(t);
+        const int32_t b = c.sequence_of(t);
         if (n == t) mine = b;
     }
     return mine;
@@ -204,7 +204,11 @@ constexpr int kRor4 = 0x124, kRor8 = 0x128;         // rotations of 16 lanes
 __device__ inline uint32_t high_part(float v) { return __builtin_bit_cast(uint32_t, v) & 0xffff0000u; }
 __device__ inline float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
 __device__ inline uint32_t pack_high(float lo, float hi) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u); }
-__device__ inline uint32_t pack_bf16(float lo, float hi) { return ppmm::from_f32<BF16>(lo) | (uint32_t)ppmm::from_f32<BF16>(hi) << 16; }
+__device__ inline uint32_t pack_bf16(float lo, float hi)
+{
+    typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, Pair{(__bf16)lo, (__bf16)hi});
+}
 
 // 64 lanes' 16 or 4 bytes from memory to neighbouring places in LDS, without a register in between
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
@@ -607,7 +611,7 @@ __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int3
     __shared__ float part_sums[4][D];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t row = blockIdx.x, n = row / heads;
-    const int32_t b = c.sequence_of_wave(n);
+    const int32_t b = c.sequence_of(n);
     if (b < 0 || n - c.starts[b] >= max_q) return;              // the whole work-group
     const int64_t held = c.lens[b] < c.capacity() ? c.lens[b] : c.capacity(), part = split_size(held, splits, unit);
     const int used = held > part ? (int)((held + part - 1) / part) : 1;

@@ -74,19 +74,9 @@ struct Cache {
     __device__ int64_t page_bytes() const { return (int64_t)page_size * (head_dim + head_dim / 4); }
     __device__ int64_t capacity() const { return (int64_t)table_width * page_size; }
 
-    // sequence of row n, or -1.  The last b with starts[b] <= n; what does not ascend finds no sequence or one that holds n.
+    // sequence of row n, the same for the whole wave, or -1: 64 places at a time.  The last b with starts[b] <= n; where the starts do
+    // not ascend, none or one that holds n.
     __device__ int32_t sequence_of(int64_t n) const
-    {
-        int32_t lo = 0, hi = batch;             // invariant for ascending starts: starts[lo] <= n < starts[hi]
-        while (hi - lo > 1) {
-            const int32_t mid = lo + (hi - lo) / 2;
-            if (starts[mid] <= n) lo = mid; else hi = mid;
-        }
-        return starts[lo] <= n && n < starts[lo + 1] ? lo : -1;
-    }
-
-    // The same for a wave that looks for one row together: 64 places at a time.
-    __device__ int32_t sequence_of_wave(int64_t n) const
     {
         const int lane = threadIdx.x % 64;
         int32_t lo = 0;
