@@ -82,6 +82,64 @@ def _too_early(body):
             todo += [(k, slots + 1) for k in after(j)]
 
 
+def _short_waits(body):
+    """Written waits s_waitcnt vmcnt(N > 0) and, where that is below N, the fewest loads between one and a load to LDS in front of it.
+
+    Such a wait is for the loads to LDS, with N later loads of weights left under way: were they fewer, it would end too early."""
+    code, labels, written, inside = [], {}, [], False
+    for line in body.split("\n"):
+        inside = "#ASMSTART" in line or inside and "#ASMEND" not in line
+        line = line.split(";")[0].strip()
+        label = re.match(r"(\.LBB\S+):", line)
+        if label:
+            labels[label.group(1)] = len(code)
+        elif line and not line.startswith(".") and not line.endswith(":"):
+            code.append(line)
+            written.append(inside)
+    before = [[] for _ in code]
+    for i, line in enumerate(code):
+        op, _, operands = line.partition(" ")
+        to = [] if op in ("s_endpgm", "s_branch") else [i + 1]
+        to += [labels[operands.strip()]] if op == "s_branch" or op.startswith("s_cbranch") else []
+        for j in to:
+            if j < len(code):
+                before[j].append(i)
+    for i, line in enumerate(code):
+        wait = re.match(r"s_waitcnt vmcnt\((\d+)\)", line)
+        if not wait or not written[i] or int(wait.group(1)) == 0:
+            continue
+        left, seen, todo, least = int(wait.group(1)), {}, [(j, 0) for j in before[i]], None
+        while todo:
+            j, loads = todo.pop()
+            if seen.get(j, left) <= loads:
+                continue
+            seen[j] = loads
+            if re.match(r"(global|buffer)_load", code[j]):
+                if re.search(r"\blds\b|_lds_", code[j]):
+                    least = loads if least is None else min(least, loads)
+                    continue
+                loads += 1
+            todo += [(k, loads) for k in before[j]]
+        yield left, least
+
+
+def test_the_check_of_waits_sees_what_it_should():
+    dma, load = "buffer_load_dwordx4 v1, s[0:3], 0 offen lds\n", "global_load_dwordx4 v[2:5], v[6:7], off\n"
+    wait = ";;#ASMSTART\ns_waitcnt vmcnt(2)\n;;#ASMEND\ns_endpgm\n"
+    assert list(_short_waits(dma + load + load + wait)) == [(2, None)]
+    assert list(_short_waits(dma + load + wait)) == [(2, 1)]
+    assert list(_short_waits(dma + load + "s_cbranch_scc1 .LBB0_1\n" + load + ".LBB0_1:\n" + wait)) == [(2, 1)]
+
+
+def test_waits_for_lds_leave_no_more_loads_than_follow(kernels):
+    counted = 0
+    for name, body in kernels.items():
+        for left, least in _short_waits(body):
+            counted += 1
+            assert least is None, (name, left, least)
+    assert counted > 100 or not any("many_tokens" in name for name in kernels)
+
+
 def test_the_check_sees_what_it_should():
     mfma = "v_mfma_f32_16x16x32_f16 v[14:17], v[2:5], v[26:29], v[14:17]\n"
     assert list(_too_early(mfma + "s_cbranch_scc1 .LBB0_1\ns_nop 7\n.LBB0_1:\nv_fma_f32 v10, v34, v14, v10\ns_endpgm\n"))
