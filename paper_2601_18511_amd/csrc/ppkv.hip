@@ -240,6 +240,10 @@ struct Rows {
     }
 };
 
+// A row's result.  Without keys both sums are zero, and so is the row; where all keys are NaN no maximum was found and l is zero
+// too, but not v.
+template <class T> __device__ inline uint16_t divided(float v, float l) { return ppmm::from_f32<T>(v / (l == 0.0f ? 1.0f : l)); }
+
 // Keys of one split: a multiple of unit, which is whole rounds of the four waves.
 __device__ inline int64_t split_size(int64_t length, int splits, int unit)
 {
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
             const int64_t n = rows.token(r);
             if (r >= count || n < 0 || n >= tokens) continue;
             const int head = rows.kv_head * rows.G + (int)(r % rows.G);
-            if (splits == 1) out[n * ots + head * ohs + ch] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : v / l);
+            if (splits == 1) out[n * ots + head * ohs + ch] = divided<T>(v, l);
             else {
                 float *to = scratch + ((n * heads + head) * splits + split) * (D + 2);
                 to[ch] = v;
@@ -645,7 +649,7 @@ __global__ __launch_bounds__(256) void join_kernel(Cache c, int64_t tokens, int3
     const int ch = threadIdx.x;
     if (ch < D) {
         const float sum = part_sums[0][ch] + part_sums[1][ch] + part_sums[2][ch] + part_sums[3][ch];
-        out[n * ots + row % heads * ohs + ch] = ppmm::from_f32<T>(l == 0.0f ? 0.0f : sum / l);
+        out[n * ots + row % heads * ohs + ch] = divided<T>(sum, l);
     }
 }
 

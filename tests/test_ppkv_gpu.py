@@ -291,6 +291,21 @@ def test_what_is_not_attended_to_has_no_part(gpu_device, dtype):
                     assert torch.isnan(hit[..., 32:]).all() and torch.equal(hit[..., :32], clean[row:, 2:, :32])
 
 
+@pytest.mark.parametrize("D", (64, 128))
+def test_rows_that_attend_to_nothing_but_nan(gpu_device, D):
+    """Every key that a row attends to is a NaN: the row is NaN, not the zeros of a row without keys; one token, a tile, several splits."""
+    import torch
+
+    for t, n, max_len in ((1, 1, 0), (1, 64, 0), (1, 3000, 3000), (40, 90, 0), (3, 2, 0)):
+        b = Batch([(t, n)], 4, 2, D, 16, "bfloat16", gpu_device, seed=12)
+        b.k[0][:, 0, 5] = float("nan")
+        out = _attend(b.fill(), max_len=max_len).cpu()
+        empty = max(t - n, 0)                                               # causal rows in front of the first token
+        assert (out[:empty] == 0).all()
+        assert torch.isnan(out[empty:, :2]).all(), (t, n)
+        assert not torch.isnan(out[:, 2:]).any()
+
+
 def test_bad_pages_and_lengths_stay_inside(gpu_device):
     """Page numbers outside the pool, lengths beyond the table and below zero, starts that do not ascend: nothing is written outside,
     such tokens are not attended to."""
