@@ -226,17 +226,18 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(Weights a, Weights 
     finish<T, kWaves, kGated>(part, tile, M, tokens, y, ldy);
 }
 
-// Up to sixteen tokens of any length; x comes from the caches as the matrix instruction wants it.
+// Sixteen tokens of any length a work-group; x comes from the caches as the matrix instruction wants it.
 template <class T, int kWaves, int kGroups, bool kGated, bool kOffsets>
-__global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t tokens,
-                                                                 const uint16_t *x, int64_t ldx, uint16_t *y, int64_t ldy)
+__global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weights b, int64_t M, int64_t K, int kblocks, int64_t all_tokens,
+                                                                 const uint16_t *all_x, int64_t ldx, uint16_t *all_y, int64_t ldy)
 {
     constexpr int kMats = kGated ? 2 : 1;
     using Par = Params<kGroups, kOffsets>;
     __shared__ f32x4 part[kWaves][kMats][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), h = lane / 16, col = lane % 16;
-    const int64_t tile = blockIdx.x;
-    const uint16_t *row = x + col * ldx;
+    const uint32_t tiles = (uint32_t)((M + 15) / 16);       // of rows; the next tokens come behind them all
+    const int64_t tile = blockIdx.x % tiles, t0 = (int64_t)(blockIdx.x / tiles) * 16, tokens = all_tokens - t0;
+    const uint16_t *row = all_x + (t0 + col) * ldx;
     u32x4 codes[kMats];
     Par params[kMats];
     const auto fetch = [&](int kb) __attribute__((always_inline)) {
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_tokens_kernel(Weights a, Weig
 #pragma unroll
     for (int w = 0; w < kMats; ++w) part[wave][w][lane] = sum[w][0];
     __syncthreads();
-    finish<T, kWaves, kGated>(part, tile, M, tokens, y, ldy);
+    finish<T, kWaves, kGated>(part, tile, M, tokens, all_y + t0 * ldy, ldy);
 }
 
 // ---- a batch of tokens ---------------------------------------------------------------------------------------------
@@ -563,8 +564,8 @@ template <class T, int kGroups, bool kGated> void launch_few(const Call &c)
     const ppmv_plan *p = c.p, *u = c.u;
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
     auto kernel = p->has_offsets ? few_tokens_kernel<T, 8, kGroups, kGated, true> : few_tokens_kernel<T, 8, kGroups, kGated, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((p->M + 15) / 16)), dim3(64 * 8), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, c.y,
-                       c.ldy);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p->M + 15) / 16 * ((c.T + 15) / 16))), dim3(64 * 8), 0, c.stream, a, b, p->M, p->K,
+                       (int)((p->K + 127) / 128), c.T, c.x, c.ldx, c.y, c.ldy);
 }
 
 template <class T, int kWaves, int kGroups, bool kGated> void launch_stream(const Call &c)
@@ -622,8 +623,10 @@ template <class T, int kGroups, bool kGated> void launch(const Call &c)
         }
         return launch_stream<T, 8, kGroups, kGated>(c);
     }
-    // 16 tokens: 4096 -> 4096 6.3 us and 7.3 with x shared by two waves, 4096 -> 14336 gated 21.9 and 15.5 by four
-    if (c.T <= 16 && tiles * mats <= 512) return launch_few<T, kGroups, kGated>(c);
+    // Sixteen tokens a work-group while there is no more than one for a compute unit: 64 tokens 4096 -> 1024 6.5 us and 11.9 with x shared
+    // by two waves, gated 7.2 and 15.2; with two for each the gain is gone (32 tokens 4096 -> 4096 10.8 and 8.9).  Up to 16 tokens
+    // also with two: there is no x to share.  4096 -> 14336 gated 21.9 and, x shared by four, 15.5.
+    if (tiles * ((c.T + 15) / 16) <= 256 || (c.T <= 16 && tiles * mats <= 512)) return launch_few<T, kGroups, kGated>(c);
     // Otherwise the least of what was measured at K = 4096 (in tenths of a microsecond; all three grow alike with K), with work-groups
     // counted in rounds of the chip: x shared by two waves or by four, or large tiles.
     const int64_t chunks = c.T <= 64 ? 1 : (c.T + 63) / 64, large = (tiles * mats + 7) / 8 * ((c.T + 127) / 128);

@@ -272,3 +272,43 @@ def test_streams_and_graphs(gpu_device, T):
         torch.cuda.synchronize()
         pkg.ppmv_gated_run(plan, plan, new, eager)
         assert torch.equal(dst, want[i % 2]) and torch.equal(gated, eager)
+
+
+# M, K, T, group: more rows than sixteen tokens a work-group are taken for; x shared by two waves (16 to 64 tokens and more than
+# one such batch) and by four, and large tiles
+BATCHES = [(2100, 1000, 20, 64), (2100, 333, 40, 32), (2051, 640, 57, 128), (2100, 264, 150, 32), (13000, 200, 20, 128), (13000, 136, 40, 32),
+           (13000, 328, 64, 64), (8300, 300, 9, 64), (12400, 300, 300, 64), (12400, 392, 300, 32), (12400, 264, 300, 128)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", (False, True))
+@pytest.mark.parametrize("M,K,T,group", BATCHES)
+def test_batches_of_tokens_and_many_rows(gpu_device, M, K, T, group, gated, dtype):
+    """Against the oracle, with rows aligned to 16 bytes and to two only; nothing beside the result is written, and a token that is
+    not finite spoils no other's results."""
+    import torch
+
+    import paper_2601_18511_amd as pkg
+
+    for offsets in (False, True):
+        codes, scales, off, x = _case(M, K, T, group, dtype, offsets, M + K + T, gpu_device)
+        plan = _plan(codes, scales, off, K, group, gpu_device)
+        want, bound = _want(codes, scales, off, x, group)
+        if gated:
+            bound = 2.2 * bound * (np.abs(want) + bound + 1) + np.abs(want * want) * (np.abs(want) + 8) * 2.0 ** -22
+            want = oracle.silu(want) * want
+        for lead, ldx, ldy in ((0, -(-K // 8) * 8, M), (1, K + 3, M + 5)):
+            xs = torch.full((T * ldx + 16,), float("nan"), dtype=x.dtype, device=gpu_device)
+            ys = torch.full((T * ldy + 16,), 77.0, dtype=x.dtype, device=gpu_device)
+            xv, yv = xs[lead:lead + T * ldx].view(T, ldx)[:, :K], ys[lead:lead + T * ldy].view(T, ldy)[:, :M]
+            xv.copy_(x)
+            run = (lambda: pkg.ppmv_gated_run(plan, plan, xv, yv)) if gated else (lambda: pkg.ppmv_run(plan, xv, yv))
+            run()
+            _near(yv, want, bound, dtype)
+            clean = yv.clone()
+            assert (ys[:lead] == 77).all() and (ys[lead + T * ldy:] == 77).all()
+            assert (ys[lead:lead + T * ldy].view(T, ldy)[:, M:] == 77).all()
+            xv[T - 2, K - 1] = float("nan")
+            run()
+            assert torch.isnan(yv[T - 2]).all()
+            assert torch.equal(yv[:T - 2], clean[:T - 2]) and torch.equal(yv[T - 1], clean[T - 1])
