@@ -11,7 +11,9 @@
  * stride given in elements; elements are aligned to their size, nothing more is asked for.  Calls are asynchronous on the
  * given stream (NULL = default stream), allocate nothing and keep nothing between calls, so any number of runs of one plan
  * or one cache may overlap as long as no call writes what another one reads or writes; all of them can be captured into a
- * graph.  Sums are held in 32-bit floating point; results are rounded once, to nearest even.  No function throws or aborts.
+ * graph.  Sums are held in 32-bit floating point; results are rounded once, to nearest even.  One factor has fewer bits: what
+ * attention weighs a value with, its scale times the exponential of its score, is rounded to 16 bits or more.  No function throws or
+ * aborts.
  */
 #ifndef PPMM_H
 #define PPMM_H

@@ -170,12 +170,16 @@ __global__ __launch_bounds__(kThreads) void read_kernel(Cache c, int64_t tokens,
 // Tiles of 64 keys, 16 at a time as the rows of a matrix product with queries as its columns.  Nothing is dequantised:
 //
 //   score     sum_j s_j (sum_{c in j} q_c (16 + code_c))  +  sum_j b_j sum_{c in j} q_c
-//   output    sum_i (p_i s_ij) (16 + code_ic)             +  sum_i p_i b_ij              for a channel c of group j
+//   output    sum_i (p_i s_ij) (16 + code_ic - 24)        +  sum_i p_i (b_ij + 24 s_ij)  for a channel c of group j
 //
-// q (16 + code) is exact; p s enters in two bf16 halves of 8 bits each.  A key's scales and offsets are 16 bytes, which are an
-// operand of the matrix instruction as they are: times a one they come out in the layout of the scores, times the groups' sums of q (in
-// three bf16 parts) they are the score's second sum.  The values' codes go through LDS, whose transposing read hands a lane
-// sixteen keys of one channel.  The sixteen keys are those whose scores the lane holds, so probabilities stay where they are.
+// q (16 + code) is exact.  p s enters as two bf16 numbers, rounded to 16 bits or more, and -24 p s as the same numbers' product with
+// -24: what their rounding leaves out is weighed with code - 8.  Every tile's sum starts with it, so that no sum grows by 24 p s, which the
+// offsets would take off again only at the end: of 3968 tokens' results in bf16 2.5 % were not the nearest number to the exact one
+// without it (and with the first number cut instead of rounded), 0.26 % are; 564 and 620 us.  Three bf16 parts, all bits of p s: 0.18 %, 654 us.
+// A key's scales and offsets are 16 bytes, which are an operand of the matrix instruction as they are: times a one (and 24 for the
+// scale beside its offset) they come out in the layout of the scores, times the groups' sums of q (in three bf16 parts) they are the
+// score's second sum.  The values' codes go through LDS, whose transposing read hands a lane sixteen keys of one channel.  The sixteen
+// keys are those whose scores the lane holds, so probabilities stay where they are.
 //
 // Few queries (kFew): a column is a pair of group and query, 16 / (D/32) queries a tile: the products of all groups with their
 // scales are one instruction each, and lanes do not work on empty columns.  Otherwise a column is a query, and the groups follow one
@@ -203,8 +207,7 @@ constexpr int kRor4 = 0x124, kRor8 = 0x128;         // rotations of 16 lanes
 
 __device__ inline uint32_t high_part(float v) { return __builtin_bit_cast(uint32_t, v) & 0xffff0000u; }
 __device__ inline float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
-__device__ inline uint32_t pack_high(float lo, float hi) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u); }
-__device__ inline uint32_t pack_bf16(float lo, float hi)
+__device__ inline uint32_t pack_bf16(float lo, float hi)       // to nearest even
 {
     typedef __bf16 Pair __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, Pair{(__bf16)lo, (__bf16)hi});
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
             qsum[t][(kGroups + j) / 2] |= (kGroups + j) % 2 ? p : p >> 16;
         }
     }
-    // ones that bring out a scale and an offset: of the column's group, or of every group in all columns
+    // ones that bring out a scale, and an offset with 24 scales: of the column's group, or of every group in all columns
     constexpr int kSums = kFew ? 1 : kGroups;
     u32x4 one_s[kSums], one_b[kSums];
 #pragma unroll
@@ -326,6 +329,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         for (int j = 0; j < kGroups; ++j)
             if (h == 0 && (kFew ? mine == j : n == j)) {
                 one_s[n][j / 2] = j % 2 ? 0x3f800000u : 0x3f80u;
+                one_b[n][j / 2] = j % 2 ? 0x41c00000u : 0x41c0u;
                 one_b[n][(kGroups + j) / 2] = (kGroups + j) % 2 ? 0x3f800000u : 0x3f80u;
             }
     }
@@ -513,27 +517,35 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
         }
         const int token = 16 * (col / 4) + 4 * h + col % 4;      // whose values this lane hands in
         const uint8_t *from = (const uint8_t *)now.values + token * (D / 2);
-        const auto add_values = [&](int n, const u32x4 (&big)[kTiles][2], const u32x4 (&small)[kTiles][2]) __attribute__((always_inline)) {
+        const auto add_values = [&](int n, const u32x4 (&weights)[2][kTiles][2], const f32x4 (&start)[kTiles]) __attribute__((always_inline)) {
             typedef int v2i __attribute__((ext_vector_type(2)));
             const v2i w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i *)(from + 16 * (n / 2 ^ h % (D / 32)) + 8 * (n % 2)));
             const u32x4 v0 = unpack_values.get<0>((uint32_t)w[0]), v1 = unpack_values.get<0>((uint32_t)w[1]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                o[t][n] = BF16::mma(v0, big[t][0], o[t][n]);
-                o[t][n] = BF16::mma(v1, big[t][1], o[t][n]);
-                o[t][n] = BF16::mma(v0, small[t][0], o[t][n]);
-                o[t][n] = BF16::mma(v1, small[t][1], o[t][n]);
+                f32x4 acc = start[t];
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    acc = BF16::mma(v0, weights[part][t][0], acc);
+                    acc = BF16::mma(v1, weights[part][t][1], acc);
+                }
+                o[t][n] += acc;
             }
         };
-        // p times scale in two halves, and p times offset
-        const auto weigh = [&](int t, int n, const f32x4 (&sj)[4], const f32x4 (&bj)[4], u32x4 (&big)[2], u32x4 (&small)[2]) __attribute__((always_inline)) {
+        // p times scale in two parts, and p times (offset + 24 scale)
+        const auto weigh = [&](int t, int n, const f32x4 (&sj)[4], const f32x4 (&bj)[4], u32x4 (&weights)[2][kTiles][2]) __attribute__((always_inline)) {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = p[t][2 * half][e] * sj[2 * half][e], y = p[t][2 * half + 1][e] * sj[2 * half + 1][e];
-                    big[half][e] = pack_high(x, y);
-                    small[half][e] = pack_bf16(x - as_float(high_part(x)), y - as_float(high_part(y)));
+                    float x = p[t][2 * half][e] * sj[2 * half][e], y = p[t][2 * half + 1][e] * sj[2 * half + 1][e];
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const uint32_t w = pack_bf16(x, y);
+                        weights[part][t][half][e] = w;
+                        x -= as_float(w << 16);
+                        y -= as_float(w & 0xffff0000u);
+                    }
                     z[t][n] = fmaf(p[t][2 * half][e], bj[2 * half][e], z[t][n]);
                     z[t][n] = fmaf(p[t][2 * half + 1][e], bj[2 * half + 1][e], z[t][n]);
                 }
@@ -546,11 +558,21 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(Cache c, int64_t toke
                 s[i] = BF16::mma(operand<kGroups>(vp[i]), one_s[n], f32x4{0, 0, 0, 0});
                 off[i] = BF16::mma(operand<kGroups>(vp[i]), one_b[n], f32x4{0, 0, 0, 0});
             }
-            u32x4 big[kTiles][2], small[kTiles][2];
+            u32x4 weights[2][kTiles][2];
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) weigh(t, n, s, off, big[t], small[t]);
+            for (int t = 0; t < kTiles; ++t) weigh(t, n, s, off, weights);
+            const u32x4 minus24 = {BF16::kMinus24, BF16::kMinus24, BF16::kMinus24, BF16::kMinus24};
+            f32x4 start[kTiles];                    // the small parts first: their roundings are small then
 #pragma unroll
-            for (int k = 0; k < kChannelTiles / kSums; ++k) add_values(n * (kChannelTiles / kSums) + k, big, small);
+            for (int t = 0; t < kTiles; ++t) {
+                start[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int part = 1; part >= 0; --part)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) start[t] = BF16::mma(minus24, weights[part][t][half], start[t]);
+            }
+#pragma unroll
+            for (int k = 0; k < kChannelTiles / kSums; ++k) add_values(n * (kChannelTiles / kSums) + k, weights, start);
         }
     }
 
