@@ -157,8 +157,8 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
  *   heads            a multiple of kv_heads, heads / kv_heads <= 65536; max_q heads / kv_heads below 2^31 - 64
  *   max_q            no sequence has more new tokens; rows beyond are left as they were
  *   max_len          expected largest lens[b], for the division of the work only (0: table_width * page_size)
- *   scratch          device, ppkv_attention_scratch_bytes(same sizes) bytes, aligned to 16 bytes, for this call alone until
- *                    it has finished; need not be cleared; may be NULL where that is 0
+ *   scratch          device, ppkv_attention_scratch_bytes(same sizes) bytes, at most 2^27, aligned to 16 bytes, for this call alone
+ *                    until it has finished; need not be cleared; may be NULL where that is 0
  */
 size_t ppkv_attention_scratch_bytes(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, int32_t heads,
                                     int32_t max_q, int64_t max_len, int32_t device);

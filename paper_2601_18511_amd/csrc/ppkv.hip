@@ -744,7 +744,7 @@ size_t ppkv_attention_scratch_bytes(const ppkv_cache *cache, const ppkv_batch *b
                                     int64_t max_len, int32_t device)
 {
     if (ppmm_host::check_attention(cache, batch, tokens, PPMM_BF16, heads, max_q, max_len, device) != PCMM_OK) return 0;
-    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len);
+    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len, tokens);
     return d.splits == 1 ? 0 : (size_t)tokens * heads * d.splits * (cache->head_dim + 2) * sizeof(float);
 }
 
@@ -758,7 +758,7 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
     if (!ppmm_host::read_strides_ok(tokens, qts, qhs) || !ppmm_host::rows_apart(tokens, heads, D, ots, ohs)) return PCMM_EINVAL;
     if (tokens == 0 || max_q == 0) return PCMM_OK;
     if (!q_dev || !out_dev || q_dev == out_dev) return PCMM_EINVAL;
-    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len);
+    const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len, tokens);
     if (d.splits > 1 && (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < ppkv_attention_scratch_bytes(cache, batch, tokens, heads, max_q, max_len, device)))
         return PCMM_EINVAL;
     const int64_t join_blocks = tokens * heads;
