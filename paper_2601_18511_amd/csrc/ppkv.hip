@@ -701,7 +701,8 @@ pcmm_status ppkv_append(const ppkv_cache *cache, const ppkv_batch *batch, int64_
 {
     const pcmm_status rc = ppmm_host::check_cache(cache, batch, tokens, device);
     if (rc != PCMM_OK) return rc;
-    if ((type != PPMM_BF16 && type != PPMM_FP16) || !ppmm_host::read_strides_ok(tokens, kts, khs) || !ppmm_host::read_strides_ok(tokens, vts, vhs)) return PCMM_EINVAL;
+    if ((type != PPMM_BF16 && type != PPMM_FP16) || !ppmm_host::read_strides_ok(tokens, kts, khs, cache->kv_heads) ||
+        !ppmm_host::read_strides_ok(tokens, vts, vhs, cache->kv_heads)) return PCMM_EINVAL;
     if (tokens == 0) return PCMM_OK;
     if (!k_dev || !v_dev) return PCMM_EINVAL;
     const int D = cache->head_dim;
@@ -755,7 +756,7 @@ pcmm_status ppkv_attention(const ppkv_cache *cache, const ppkv_batch *batch, int
     const pcmm_status rc = ppmm_host::check_attention(cache, batch, tokens, type, heads, max_q, max_len, device);
     if (rc != PCMM_OK) return rc;
     const int D = cache->head_dim;
-    if (!ppmm_host::read_strides_ok(tokens, qts, qhs) || !ppmm_host::rows_apart(tokens, heads, D, ots, ohs)) return PCMM_EINVAL;
+    if (!ppmm_host::read_strides_ok(tokens, qts, qhs, heads) || !ppmm_host::rows_apart(tokens, heads, D, ots, ohs)) return PCMM_EINVAL;
     if (tokens == 0 || max_q == 0) return PCMM_OK;
     if (!q_dev || !out_dev || q_dev == out_dev) return PCMM_EINVAL;
     const ppmm_host::Division d = ppmm_host::divide(*cache, *batch, heads, max_q, max_len, tokens);

@@ -68,15 +68,17 @@ inline pcmm_status check_cache(const ppkv_cache *c, const ppkv_batch *b, int64_t
     return PCMM_OK;
 }
 
-inline bool read_strides_ok(int64_t tokens, int64_t token_stride, int64_t head_stride)
+// neither all tokens nor all heads reach further than 2^59 elements
+inline bool read_strides_ok(int64_t tokens, int64_t token_stride, int64_t head_stride, int64_t heads = 1)
 {
-    return token_stride >= 0 && head_stride >= 0 && head_stride <= kMaxStride && token_stride <= ((int64_t)1 << 59) / (tokens > 0 ? tokens : 1);
+    const int64_t most = (int64_t)1 << 59;
+    return token_stride >= 0 && head_stride >= 0 && head_stride <= kMaxStride && head_stride <= most / heads && token_stride <= most / (tokens > 0 ? tokens : 1);
 }
 
 // no two of tokens x heads rows of D elements overlap
 inline bool rows_apart(int64_t tokens, int64_t heads, int64_t D, int64_t token_stride, int64_t head_stride)
 {
-    if (!read_strides_ok(tokens, token_stride, head_stride)) return false;
+    if (!read_strides_ok(tokens, token_stride, head_stride, heads)) return false;
     const bool token_inner = heads == 1 || (tokens > 0 && head_stride >= (tokens - 1) * token_stride + D);
     const bool head_inner = tokens <= 1 || token_stride >= (heads - 1) * head_stride + D;
     return (head_inner && (heads == 1 || head_stride >= D)) || (token_inner && (tokens <= 1 || token_stride >= D));
