@@ -66,6 +66,9 @@ def load_library() -> ctypes.CDLL:
     return lib
 
 
+_I32, _I64 = range(-1 << 31, 1 << 31), range(-1 << 63, 1 << 63)        # ctypes cuts what does not fit
+
+
 def _handle(device: int, stream) -> int:
     return _raw_stream(device) if stream is None else int(stream.cuda_stream)
 
@@ -166,7 +169,10 @@ def ppmv_gated_run(gate: PpmvPlan, up: PpmvPlan, x: torch.Tensor, h: torch.Tenso
 
 
 def ppkv_pool_bytes(pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
-    return int(load_library().ppkv_pool_bytes(int(pages), int(page_size), int(kv_heads), int(head_dim)))
+    sizes = int(pages), int(page_size), int(kv_heads), int(head_dim)
+    if sizes[0] not in _I64 or not all(x in _I32 for x in sizes[1:]):
+        return 0
+    return int(load_library().ppkv_pool_bytes(*sizes))
 
 
 class PpkvCache:
@@ -239,7 +245,10 @@ def ppkv_read(cache: PpkvCache, k: Optional[torch.Tensor], v: Optional[torch.Ten
         raise ValueError("neither k nor v is wanted")
     if k is not None and v is not None and k_is[:2] != v_is[:2]:
         raise ValueError("k and v must have the same type and shape")
-    rc = (_lib or load_library()).ppkv_read(cache._c, batch, rows, kind, int(frac_bits), *k_is[2], *v_is[2], cache.device, _handle(cache.device, stream))
+    frac_bits = int(frac_bits)
+    if frac_bits not in _I32:
+        raise ValueError("frac_bits out of range")
+    rc = (_lib or load_library()).ppkv_read(cache._c, batch, rows, kind, frac_bits, *k_is[2], *v_is[2], cache.device, _handle(cache.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_read")
 
@@ -247,7 +256,10 @@ def ppkv_read(cache: PpkvCache, k: Optional[torch.Tensor], v: Optional[torch.Ten
 def ppkv_attention_scratch_bytes(cache: PpkvCache, tokens: int, heads: int, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
                                  max_q: int, max_len: int = 0) -> int:
     batch = _batch(cache, starts, lens, table)
-    return int(load_library().ppkv_attention_scratch_bytes(cache._c, batch, int(tokens), int(heads), int(max_q), int(max_len), cache.device))
+    tokens, heads, max_q, max_len = int(tokens), int(heads), int(max_q), int(max_len)
+    if tokens not in _I64 or heads not in _I32 or max_q not in _I32 or max_len not in _I64:
+        raise ValueError("tokens, heads, max_q or max_len out of range")
+    return int(load_library().ppkv_attention_scratch_bytes(cache._c, batch, tokens, heads, max_q, max_len, cache.device))
 
 
 def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
@@ -263,6 +275,8 @@ def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts:
     if tokens != out_tokens or kind != out_kind:
         raise ValueError("q and out must have the same type and shape")
     lib, device, max_q, max_len = _lib or load_library(), cache.device, int(max_q), int(max_len)
+    if max_q not in _I32 or max_len not in _I64:
+        raise ValueError("max_q or max_len out of range")
     size = lib.ppkv_attention_scratch_bytes(cache._c, batch, tokens, heads, max_q, max_len, device)
     scratch = None
     if size:        # of the pool of the stream that uses it: whoever gets the memory next runs behind this call
