@@ -1,5 +1,6 @@
 """ctypes binding of the clear track (include/ppmm.h): products of 4-bit weights and clear activations, the 4-bit K/V cache and
-attention over it.  Same names as the C ABI, argument marshalling only; there is no CPU fallback.
+attention over it.  Same names as the C ABI, argument marshalling only; there is no CPU fallback.  Inference only: a tensor that requires a
+gradient is refused while gradients are recorded.
 """
 from __future__ import annotations
 
@@ -67,6 +68,16 @@ def load_library() -> ctypes.CDLL:
 
 
 _I32, _I64 = range(-1 << 31, 1 << 31), range(-1 << 63, 1 << 63)        # ctypes cuts what does not fit
+
+
+# a result that autograd keeps is not what it kept any more (the private name takes half the time of the public one)
+_new_version = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+
+
+def _no_gradients() -> None:
+    """For a call with a tensor that requires a gradient."""
+    if torch.is_grad_enabled():
+        raise ValueError("the clear track has no gradients: call it under torch.no_grad() or with detached tensors")
 
 
 def _handle(device: int, stream) -> int:
@@ -147,9 +158,12 @@ def ppmv_run(plan: PpmvPlan, x: torch.Tensor, y: torch.Tensor, stream=None) -> N
     Ty, py, ldy = _rows(plan, "y", y, plan.M)
     if T != Ty:
         raise ValueError("x and y must have the same number of rows")
+    if x.requires_grad or y.requires_grad:
+        _no_gradients()
     rc = (_lib or load_library()).ppmv_run(plan.handle, T, px, ldx, py, ldy, _handle(plan.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppmv_run")
+    _new_version((y,))
 
 
 def ppmv_gated_run(gate: PpmvPlan, up: PpmvPlan, x: torch.Tensor, h: torch.Tensor, stream=None) -> None:
@@ -160,9 +174,12 @@ def ppmv_gated_run(gate: PpmvPlan, up: PpmvPlan, x: torch.Tensor, h: torch.Tenso
     Th, ph, ldh = _rows(gate, "h", h, gate.M)
     if T != Th:
         raise ValueError("x and h must have the same number of rows")
+    if x.requires_grad or h.requires_grad:
+        _no_gradients()
     rc = (_lib or load_library()).ppmv_gated_run(gate.handle, up.handle, T, px, ldx, ph, ldh, _handle(gate.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppmv_gated_run")
+    _new_version((h,))
 
 
 # ---- the 4-bit K/V cache ------------------------------------------------------------------------------------------------
@@ -228,6 +245,8 @@ def ppkv_append(cache: PpkvCache, k: torch.Tensor, v: torch.Tensor, starts: torc
     v_rows, v_kind, v_at = _packed(cache, "v", v, cache.kv_heads, _TYPES)
     if rows != v_rows or kind != v_kind:
         raise ValueError("k and v must have the same type and shape")
+    if k.requires_grad or v.requires_grad:
+        _no_gradients()
     rc = (_lib or load_library()).ppkv_append(cache._c, batch, rows, kind, *k_at, *v_at, cache.device, _handle(cache.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_append")
@@ -245,12 +264,16 @@ def ppkv_read(cache: PpkvCache, k: Optional[torch.Tensor], v: Optional[torch.Ten
         raise ValueError("neither k nor v is wanted")
     if k is not None and v is not None and k_is[:2] != v_is[:2]:
         raise ValueError("k and v must have the same type and shape")
+    results = tuple(t for t in (k, v) if t is not None)
+    if any(t.requires_grad for t in results):
+        _no_gradients()
     frac_bits = int(frac_bits)
     if frac_bits not in _I32:
         raise ValueError("frac_bits out of range")
     rc = (_lib or load_library()).ppkv_read(cache._c, batch, rows, kind, frac_bits, *k_is[2], *v_is[2], cache.device, _handle(cache.device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_read")
+    _new_version(results)
 
 
 def ppkv_attention_scratch_bytes(cache: PpkvCache, tokens: int, heads: int, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
@@ -274,6 +297,8 @@ def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts:
     out_tokens, out_kind, out_at = _packed(cache, "out", out, heads, _TYPES)
     if tokens != out_tokens or kind != out_kind:
         raise ValueError("q and out must have the same type and shape")
+    if q.requires_grad or out.requires_grad:
+        _no_gradients()
     lib, device, max_q, max_len = _lib or load_library(), cache.device, int(max_q), int(max_len)
     if max_q not in _I32 or max_len not in _I64:
         raise ValueError("max_q or max_len out of range")
@@ -289,3 +314,4 @@ def ppkv_attention(cache: PpkvCache, q: torch.Tensor, out: torch.Tensor, starts:
                             1 if causal else 0, max_q, max_len, scratch.data_ptr() if size else None, size, device, _handle(device, stream))
     if rc != PCMM_OK:
         raise PcmmError(rc, "ppkv_attention")
+    _new_version((out,))
