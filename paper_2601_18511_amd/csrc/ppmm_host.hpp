@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/ppmm.h"
 
 namespace ppmm_host {
@@ -38,6 +40,42 @@ inline pcmm_status check_product(int64_t M, int64_t K, int64_t T, const void *x,
     if (T > kMaxRows || ldx > kMaxStride / T || ldy > kMaxStride / T) return PCMM_EUNSUPPORTED;
     if ((up(M, 16) / 16) * (up(T, 64) / 64) > ((int64_t)1 << 22)) return PCMM_EUNSUPPORTED;      // no launch of 2^32 threads, whatever the kernel
     return PCMM_OK;
+}
+
+// Which kernel takes a product, and in which of its forms: one for every size, so that tests see the choice without a GPU.
+struct Form {
+    enum Kernel { kStream, kFew, kBatch, kMany } kernel;
+    int waves;      // kStream: of a work-group; kBatch: waves that take rows
+    int tokens;     // kBatch: tokens of a work-group
+};
+
+// Two matrices in groups of 32 do not fit the registers of sixteen waves, nor with offsets those of a batch of more than 32 tokens.
+inline constexpr bool stream_has(int waves, bool gated, int group) { return waves == 8 || !(gated && group == 32); }
+inline constexpr bool batch_has(int tokens, bool gated, int group, bool offsets) { return tokens <= 32 || !(gated && group == 32 && offsets); }
+
+inline Form choose(int64_t M, int64_t K, int64_t T, int group, bool gated, bool offsets)
+{
+    const int64_t tiles = (M + 15) / 16, mats = gated ? 2 : 1;
+    // x in LDS: at most 30 KiB beside at most 32 KiB of the waves' sums
+    if (T <= 4 && T * K <= 14336) {
+        // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
+        // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.
+        if (M <= 8192 && K > 8192 && stream_has(16, gated, group)) return Form{Form::kStream, 16, 0};
+        return Form{Form::kStream, 8, 0};
+    }
+    // Sixteen tokens a work-group while there is no more than one for a compute unit: 64 tokens 4096 -> 1024 6.5 us and 11.9 with x shared
+    // by two waves, gated 7.2 and 15.2; with two for each the gain is gone (32 tokens 4096 -> 4096 10.8 and 8.9).  Up to 16 tokens
+    // also with two: there is no x to share.  4096 -> 14336 gated 21.9 and, x shared by four, 15.5.
+    if (tiles * ((T + 15) / 16) <= 256 || (T <= 16 && tiles * mats <= 512)) return Form{Form::kFew, 8, 16};
+    // Otherwise the least of what was measured at K = 4096 (in tenths of a microsecond; all three grow alike with K), with work-groups
+    // counted in rounds of the chip: x shared by two waves or by four, or large tiles.
+    const int64_t chunks = T <= 64 ? 1 : (T + 63) / 64, large = (tiles * mats + 7) / 8 * ((T + 127) / 128);
+    const double two = (gated ? 165 : 130) * std::max(1.0, (tiles + 1) / 2 * chunks / 256.0);
+    const double four = (gated ? 260 : 195) * std::max(1.0, (tiles + 3) / 4 * chunks / 256.0);
+    const double many = T <= 64 ? 1e30 : std::max(570.0, 1.47 * large);
+    if (many < two && many < four) return Form{Form::kMany, 4, 128};
+    const int tokens = T >= 64 ? 64 : (int)(T + 15) / 16 * 16;
+    return Form{Form::kBatch, two < four ? 2 : 4, batch_has(tokens, gated, group, offsets) ? tokens : 32};
 }
 
 // ---- cache ---------------------------------------------------------------------------------------------------------

@@ -14,7 +14,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
 #include <new>
 
 #include "ppmm_device.hpp"
@@ -593,49 +592,36 @@ template <class T, int kGroups, bool kGated> void launch_many(const Call &c)
 template <class T, int kTok, int kRowWaves, int kGroups, bool kGated> void launch_batch(const Call &c)
 {
     const ppmv_plan *p = c.p, *u = c.u;
-    // two matrices in groups of 32 with offsets: no registers for more than 32 tokens
-    if constexpr (kGated && kGroups == 4 && kTok > 2)
-        if (p->has_offsets) return launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
     const Weights a{(const u32x4 *)p->codes, p->params}, b{(const u32x4 *)u->codes, u->params};
-    auto kernel = p->has_offsets ? batch_kernel<T, kTok, kRowWaves, kGroups, kGated, true> : batch_kernel<T, kTok, kRowWaves, kGroups, kGated, false>;
+    auto kernel = batch_kernel<T, kTok, kRowWaves, kGroups, kGated, false>;
+    if constexpr (ppmm_host::batch_has(16 * kTok, kGated, 128 / kGroups, true))
+        if (p->has_offsets) kernel = batch_kernel<T, kTok, kRowWaves, kGroups, kGated, true>;
     const dim3 grid((unsigned)(((p->M + 15) / 16 + kRowWaves - 1) / kRowWaves * ((c.T + 16 * kTok - 1) / (16 * kTok))));
     hipLaunchKernelGGL(kernel, grid, dim3(64 * kBatchWaves), 0, c.stream, a, b, p->M, p->K, (int)((p->K + 127) / 128), c.T, c.x, c.ldx, buffered(c), c.y,
                        c.ldy);
 }
 
-template <class T, int kRowWaves, int kGroups, bool kGated> void launch_batches(const Call &c)
+template <class T, int kRowWaves, int kGroups, bool kGated> void launch_batches(const Call &c, int tokens)
 {
-    if (c.T <= 16) launch_batch<T, 1, kRowWaves, kGroups, kGated>(c);
-    else if (c.T <= 32) launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
-    else if (c.T <= 48) launch_batch<T, 3, kRowWaves, kGroups, kGated>(c);
+    if (tokens == 16) launch_batch<T, 1, kRowWaves, kGroups, kGated>(c);
+    else if (tokens == 32) launch_batch<T, 2, kRowWaves, kGroups, kGated>(c);
+    else if (tokens == 48) launch_batch<T, 3, kRowWaves, kGroups, kGated>(c);
     else launch_batch<T, 4, kRowWaves, kGroups, kGated>(c);
 }
 
 template <class T, int kGroups, bool kGated> void launch(const Call &c)
 {
-    const int64_t tiles = (c.p->M + 15) / 16, mats = kGated ? 2 : 1;
-    // x in LDS: at most 30 KiB beside at most 32 KiB of the waves' sums
-    if (c.T <= 4 && c.T * c.p->K <= 14336) {
-        // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
-        // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.  (Two matrices in groups of 32 do not fit the registers then.)
-        if constexpr (!(kGated && kGroups == 4)) {
-            if (c.p->M <= 8192 && c.p->K > 8192) return launch_stream<T, 16, kGroups, kGated>(c);
-        }
-        return launch_stream<T, 8, kGroups, kGated>(c);
+    using ppmm_host::Form;
+    const Form form = ppmm_host::choose(c.p->M, c.p->K, c.T, c.p->group, kGated, c.p->has_offsets);
+    if (form.kernel == Form::kMany) return launch_many<T, kGroups, kGated>(c);
+    if (form.kernel == Form::kFew) return launch_few<T, kGroups, kGated>(c);
+    if (form.kernel == Form::kBatch) {
+        if (form.waves == 2) return launch_batches<T, 2, kGroups, kGated>(c, form.tokens);
+        return launch_batches<T, 4, kGroups, kGated>(c, form.tokens);
     }
-    // Sixteen tokens a work-group while there is no more than one for a compute unit: 64 tokens 4096 -> 1024 6.5 us and 11.9 with x shared
-    // by two waves, gated 7.2 and 15.2; with two for each the gain is gone (32 tokens 4096 -> 4096 10.8 and 8.9).  Up to 16 tokens
-    // also with two: there is no x to share.  4096 -> 14336 gated 21.9 and, x shared by four, 15.5.
-    if (tiles * ((c.T + 15) / 16) <= 256 || (c.T <= 16 && tiles * mats <= 512)) return launch_few<T, kGroups, kGated>(c);
-    // Otherwise the least of what was measured at K = 4096 (in tenths of a microsecond; all three grow alike with K), with work-groups
-    // counted in rounds of the chip: x shared by two waves or by four, or large tiles.
-    const int64_t chunks = c.T <= 64 ? 1 : (c.T + 63) / 64, large = (tiles * mats + 7) / 8 * ((c.T + 127) / 128);
-    const double two = (kGated ? 165 : 130) * std::max(1.0, (tiles + 1) / 2 * chunks / 256.0);
-    const double four = (kGated ? 260 : 195) * std::max(1.0, (tiles + 3) / 4 * chunks / 256.0);
-    const double many = c.T <= 64 ? 1e30 : std::max(570.0, 1.47 * large);
-    if (many < two && many < four) return launch_many<T, kGroups, kGated>(c);
-    if (two < four) return launch_batches<T, 2, kGroups, kGated>(c);
-    launch_batches<T, 4, kGroups, kGated>(c);
+    if constexpr (ppmm_host::stream_has(16, kGated, 128 / kGroups))
+        if (form.waves == 16) return launch_stream<T, 16, kGroups, kGated>(c);
+    launch_stream<T, 8, kGroups, kGated>(c);
 }
 
 template <class T, bool kGated> void by_group(const Call &c)
