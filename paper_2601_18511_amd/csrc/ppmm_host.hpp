@@ -67,15 +67,19 @@ inline Form choose(int64_t M, int64_t K, int64_t T, int group, bool gated, bool 
     // by two waves, gated 7.2 and 15.2; with two for each the gain is gone (32 tokens 4096 -> 4096 10.8 and 8.9).  Up to 16 tokens
     // also with two: there is no x to share.  4096 -> 14336 gated 21.9 and, x shared by four, 15.5.
     if (tiles * ((T + 15) / 16) <= 256 || (T <= 16 && tiles * mats <= 512)) return Form{Form::kFew, 8, 16};
-    // Otherwise the least of what was measured at K = 4096 (in tenths of a microsecond; all three grow alike with K), with work-groups
-    // counted in rounds of the chip: x shared by two waves or by four, or large tiles.
-    const int64_t chunks = T <= 64 ? 1 : (T + 63) / 64, large = (tiles * mats + 7) / 8 * ((T + 127) / 128);
-    const double two = (gated ? 165 : 130) * std::max(1.0, (tiles + 1) / 2 * chunks / 256.0);
-    const double four = (gated ? 260 : 195) * std::max(1.0, (tiles + 3) / 4 * chunks / 256.0);
-    const double many = T <= 64 ? 1e30 : std::max(570.0, 1.47 * large);
-    if (many < two && many < four) return Form{Form::kMany, 4, 128};
-    const int tokens = T >= 64 ? 64 : (int)(T + 15) / 16 * 16;
-    return Form{Form::kBatch, two < four ? 2 : 4, batch_has(tokens, gated, group, offsets) ? tokens : 32};
+    // Otherwise the least of an estimate, in tenths of a microsecond at K = 4096 (all three grow alike with K): x shared by two waves, by
+    // four, or large tiles.  Work-groups of 16 to 64 tokens count in rounds of the chip's 256 compute units, large tiles, of which two share
+    // a compute unit, in proportion past the first 256.  Measured with 2100 to 14336 rows, 20 to 1000 tokens, all groups, with and without offsets: the
+    // choice takes 0.4 % more than the best on average and 23 % at the most (6000 rows, 700 tokens, groups of 128, gated, offsets: 159 us, 129 by four).
+    // Two matrices in groups of 32 and more than 48 tokens keep part of their values outside the registers: 27 us a round for 15.
+    const bool narrow = group == 32;
+    const int longest = T >= 64 ? 64 : (int)(T + 15) / 16 * 16, tokens = batch_has(longest, gated, group, offsets) ? longest : 32;
+    const int64_t chunks = (T + tokens - 1) / tokens, large = (tiles * mats + 7) / 8 * ((T + 127) / 128);
+    const double round = !gated ? 125 : narrow && tokens > 48 ? 270 : 150;
+    const double two = round * (((tiles + 1) / 2 * chunks + 255) / 256), four = 1.55 * round * (((tiles + 3) / 4 * chunks + 255) / 256);
+    const double many = (580.0 + std::max<int64_t>(0, large - 256)) * (offsets ? 1.25 : 1.0) * (narrow ? 1.25 : 1.0);
+    if (T > 64 && many < two && many < four) return Form{Form::kMany, 4, 128};
+    return Form{Form::kBatch, two < four ? 2 : 4, tokens};
 }
 
 // ---- cache ---------------------------------------------------------------------------------------------------------

@@ -10,10 +10,10 @@ from oracle import clear_oracle as oracle
 CASES = [(40, 2500, 1), (33, 1100, 4),                     # x in LDS, 8 waves
          (40, 14336, 1), (33, 8200, 1),                    # 16 waves (two matrices in groups of 32: 8)
          (100, 700, 7), (520, 1100, 100), (2050, 264, 16),  # 16 tokens a work-group
-         (8300, 1160, 9), (4200, 1160, 9),                 # x shared by two waves, 16 tokens (plain; gated)
+         (20000, 1160, 9), (4200, 1160, 9),                # x shared by two waves, 16 tokens (plain; gated)
          (2100, 1160, 30), (2100, 1160, 45), (2100, 1160, 60), (2100, 1160, 70), (2100, 2184, 130),
          (13000, 1160, 9), (13000, 1160, 30), (13000, 1160, 45), (13000, 1160, 60), (20000, 264, 70),      # by four
-         (12400, 392, 300), (6300, 264, 500)]              # large tiles
+         (12400, 392, 300), (6300, 264, 500), (2100, 264, 4000)]        # large tiles
 
 
 def forms(M, K, T):
