@@ -2,9 +2,10 @@
  * ppmm.h - C ABI of the clear track: products of plaintext weights and clear activations, the public K/V cache and
  * attention over it, all held in 4 bits.  Part of the same library as pcmm.h, with its status codes and conventions.
  *
- * A mixed prompt (Section 4.1) has a public prefix and an encrypted suffix.  The public tokens run in the clear with the
- * weights that the encrypted ones are multiplied with (Section 5.1), and leave a public K/V cache, which the encrypted
- * track reads as the plaintext operand of PC-attention (Section 4.2).  The converted weights of the encrypted track fill
+ * A mixed prompt (Section 4.1) has a public prefix and an encrypted suffix.  The public tokens run in the clear through the
+ * layers whose weights the encrypted ones are multiplied with (Section 5.1), and leave a public K/V cache, which the encrypted
+ * track reads as the plaintext operand of PC-attention (Section 4.2).  Codes and scales are the caller's: nothing here makes
+ * them of the integers of a pcmm_plan, or integers of them.  The converted weights of the encrypted track fill
  * most of the memory (Section 5.3), so here a weight, a key or a value takes 4 bits and its share of a group's scale.
  *
  * Conventions.  "device" pointers are HIP device memory on the device that is named.  Matrices are row-major with the row
@@ -127,7 +128,8 @@ typedef struct {
  *   type                   PPMM_BF16 or PPMM_FP16
  *   tokens                 rows of k_dev and v_dev, 0 <= tokens < 2^31
  *
- * No two tokens of one call may have the same place in the cache.  PCMM_EINVAL for null pointers and sizes out of range.
+ * No two tokens of one call may have the same place in the cache.  PCMM_EINVAL for null pointers, sizes and strides out of range;
+ * PCMM_EUNSUPPORTED, here and in ppkv_read, for tokens kv_heads head_dim above 2^34 - 1024.
  */
 pcmm_status ppkv_append(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, ppmm_type type, const void *k_dev,
                         int64_t k_token_stride, int64_t k_head_stride, const void *v_dev, int64_t v_token_stride,
@@ -151,7 +153,8 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
  *
  * over the tokens i of the row's sequence, i < lens[b], and, if causal, i not behind the row's own token.  A row that
  * attends to nothing is zero.  A token behind a causal row does not reach it, whatever it holds; of the tokens that a row
- * attends to, a NaN key makes the whole row NaN, and values that read as NaN make those 32 channels of it NaN.
+ * attends to, a NaN key makes the whole row NaN, and values that read as NaN make those 32 channels of it NaN.  So may scores
+ * that 32-bit floating point does not hold, and values 2^8 times whose magnitudes it does not hold the sum of.
  *
  *   q_dev, out_dev   device, [tokens][heads][head_dim] with strides; the rows of out_dev must be apart; out_dev != q_dev
  *   heads            a multiple of kv_heads, heads / kv_heads <= 65536; max_q heads / kv_heads below 2^31 - 64
@@ -159,6 +162,9 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
  *   max_len          expected largest lens[b], for the division of the work only (0: table_width * page_size)
  *   scratch          device, ppkv_attention_scratch_bytes(same sizes) bytes, at most 2^27, aligned to 16 bytes, for this call alone
  *                    until it has finished; need not be cleared; may be NULL where that is 0
+ *
+ * PCMM_EINVAL for null pointers, sizes and strides out of range and too little scratch; PCMM_EUNSUPPORTED for 2^24 work-groups and
+ * more: batch kv_heads times a sequence's max_q heads / kv_heads rows by sixteens (at least one).
  */
 size_t ppkv_attention_scratch_bytes(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, int32_t heads,
                                     int32_t max_q, int64_t max_len, int32_t device);

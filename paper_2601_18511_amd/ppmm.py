@@ -264,8 +264,8 @@ def ppkv_read(cache: PpkvCache, k: Optional[torch.Tensor], v: Optional[torch.Ten
         raise ValueError("neither k nor v is wanted")
     if k is not None and v is not None and k_is[:2] != v_is[:2]:
         raise ValueError("k and v must have the same type and shape")
-    results = tuple(t for t in (k, v) if t is not None)
-    if any(t.requires_grad for t in results):
+    results = (v,) if k is None else (k,) if v is None else (k, v)
+    if results[0].requires_grad or results[-1].requires_grad:
         _no_gradients()
     frac_bits = int(frac_bits)
     if frac_bits not in _I32:
