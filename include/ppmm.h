@@ -165,6 +165,9 @@ pcmm_status ppkv_read(const ppkv_cache *cache, const ppkv_batch *batch, int64_t 
  *
  * PCMM_EINVAL for null pointers, sizes and strides out of range and too little scratch; PCMM_EUNSUPPORTED for 2^24 work-groups and
  * more: batch kv_heads times a sequence's max_q heads / kv_heads rows by sixteens (at least one).
+ *
+ * The last bits of a result may depend on the sizes of the call, not on what else is in the batch.  The work of every sequence is divided
+ * by max_q and max_len alike: a prompt and single tokens are better given in two calls.
  */
 size_t ppkv_attention_scratch_bytes(const ppkv_cache *cache, const ppkv_batch *batch, int64_t tokens, int32_t heads,
                                     int32_t max_q, int64_t max_len, int32_t device);

@@ -56,7 +56,8 @@ inline constexpr bool batch_has(int tokens, bool gated, int group, bool offsets)
 inline Form choose(int64_t M, int64_t K, int64_t T, int group, bool gated, bool offsets)
 {
     const int64_t tiles = (M + 15) / 16, mats = gated ? 2 : 1;
-    // x in LDS: at most 30 KiB beside at most 32 KiB of the waves' sums
+    // x in LDS: 28 KiB, at most 30 with K filled up to 128 and the odd pitch, beside at most 32 KiB of the waves' sums; what a larger
+    // share would do for 2 to 4 tokens of a K that just misses it (4 tokens of 4096) is not measured
     if (T <= 4 && T * K <= 14336) {
         // with no more than two work-groups a compute unit and a long contraction, twice the waves: 14336 -> 4096 10.0 -> 7.8 us;
         // 4096 -> 4096 3.5 and 3.7 us, 4096 -> 14336 12.3 and 13.9 us.
